@@ -302,6 +302,92 @@ int compass_sequential(const compass_problem *p, const compass_links *links, voi
 int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void *C,
                          const float *P, void *stream);
 
+/* ---- the ends of a model around the tensor-parallel MLP --------------------
+ * Operators of a sequence- and vocabulary-parallel training step on one rank:
+ * cross entropy from hidden states, layer norm, embedding, each with its
+ * gradient. They take device pointers, allocate nothing, keep nothing between
+ * calls and share no state, so calls on different streams may overlap (each
+ * with a workspace of its own) and all of them may be captured in a HIP graph.
+ * A workspace may be used again by the next call on the same stream; its
+ * contents need not be initialised. Element types: COMPASS_BF16 or COMPASS_F32.
+ * Argument errors (COMPASS_ERR_INVALID, COMPASS_ERR_UNSUPPORTED) and a device
+ * other than gfx950 (COMPASS_ERR_UNSUPPORTED) are found before anything is
+ * enqueued; COMPASS_ERR_HIP when a launch fails. All results are the same bits
+ * on every call with the same operands. */
+#define COMPASS_BF16 0
+#define COMPASS_F32  1
+
+/* Softmax cross entropy over one rank's share of a vocabulary, from hidden
+ * states H (M x K bf16) and the output weight's rows W (V x K bf16) that hold
+ * the vocabulary ids [v0, v0 + V):
+ *   z = H W^T,  lse[m] = log sum_v exp z[m][v],  tlogit[m] = z[m][target[m] - v0]
+ * (0 when the target is not in the shard), loss[m] = lse[m] - tlogit[m]. The
+ * logits are never stored. target: M ids of the whole vocabulary, 64-bit; a row
+ * with a negative target has loss 0 and gradient 0. Products accumulate in
+ * fp32; lse, tlogit and loss are fp32.
+ *
+ * compass_xent_workspace: bytes of the workspace of compass_xent_forward
+ *   (backward = 0) or of compass_xent_backward with this `piece` (backward = 1).
+ * compass_xent_forward: lse, tlogit and loss (M each). With the whole vocabulary
+ *   on one rank (v0 = 0, V = its size) these are final; loss may be NULL. With
+ *   n ranks, lse and tlogit are exchanged and compass_xent_join gives the rest.
+ * compass_xent_join: from lse_parts and tlogit_parts (n x M, rank after rank),
+ *   lse[m] = log sum_q exp lse_parts[q][m], loss[m] = lse[m] - sum_q tlogit_parts[q][m].
+ * compass_xent_backward: with the whole vocabulary's lse and grad[m] the
+ *   derivative of the final result by loss[m],
+ *     dz[m][v] = grad[m] (exp(z[m][v] - lse[m]) - [v0 + v = target[m]])
+ *   dH = dz W (M x K bf16, this shard's share: to be summed over the ranks) and
+ *   dW = dz^T H (V x K bf16). z is computed again, dz held in bf16 (it enters
+ *   the matrix cores in that type: at most 2^-8 relative per element, which
+ *   does not accumulate) for one piece of `piece` vocabulary rows at a time (0: the
+ *   library's choice, at most 512 MiB of dz); sums over pieces stay in fp32.
+ *
+ * H, W, dH, dW and the workspace are 16-byte aligned and packed; none may
+ * overlap another. Limits: K a multiple of 8 up to 2^17, M up to 2^20, V up to
+ * 2^24. */
+int compass_xent_workspace(int M, int V, int K, int backward, int piece, size_t *bytes);
+int compass_xent_forward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0,
+                         float *lse, float *tlogit, float *loss, void *workspace, size_t workspace_bytes,
+                         void *stream);
+int compass_xent_join(int n, int M, const float *lse_parts, const float *tlogit_parts, const int64_t *target,
+                      float *lse, float *loss, void *stream);
+int compass_xent_backward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0,
+                          const float *lse, const float *grad, void *dH, void *dW, int piece, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/* Layer norm over rows of N elements (at most 16384):
+ *   mean = sum x / N, rstd = 1 / sqrt(sum (x - mean)^2 / N + eps),
+ *   y = (x - mean) rstd gamma + beta
+ * x, y, dy, dx: M rows of type dtype, ld elements apart (>= N). gamma, beta: N
+ * elements of type ptype, or NULL (ones, zeros). mean, rstd: M fp32. All sums
+ * are fp32; y may be x. Backward, with a = dy gamma and xh = (x - mean) rstd:
+ *   dx = rstd (a - sum(a) / N - xh sum(a xh) / N),
+ *   dgamma = sum over rows of dy xh, dbeta = sum over rows of dy (N fp32 each;
+ * NULL: not wanted, and without both no workspace is needed). dx may be dy or x. */
+int compass_norm_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *gamma,
+                         const void *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd, void *stream);
+int compass_norm_workspace(int M, int N, size_t *bytes);
+int compass_norm_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                          const void *gamma, const float *mean, const float *rstd, void *dx, int64_t lddx,
+                          float *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Embedding over one rank's table rows, the vocabulary ids [v0, v0 + V):
+ *   y[t] = scale table[ids[t] - v0], zeros for an id outside the shard
+ * (or negative: padding). ids: T 64-bit; table (V rows, ldt elements apart) and
+ * y (T rows, ldy apart): K elements of one type, rounded once.
+ * Gradient: dtable[v] = scale sum over {t : ids[t] = v0 + v} of dy[t], summed in
+ * fp32 in an order fixed by the operands alone. dy of type dtype, dtable of type
+ * gtype. accumulate = 0 writes every row of dtable; accumulate = 1 adds to the
+ * rows that have tokens and leaves the others untouched (a table tied to the
+ * output weight, whose gradient compass_xent_backward wrote). Limits: T up to
+ * 2^20, V up to 2^24, K up to 2^20. */
+int compass_embed_forward(int T, int V, int K, int dtype, const int64_t *ids, int64_t v0, const void *table,
+                          int64_t ldt, float scale, void *y, int64_t ldy, void *stream);
+int compass_embed_workspace(int T, int V, int K, size_t *bytes);
+int compass_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *ids, int64_t v0, const void *dy,
+                           int64_t ldy, float scale, void *dtable, int64_t ldt, int accumulate, void *workspace,
+                           size_t workspace_bytes, void *stream);
+
 /* Wait until the copy side of every enqueued operator has finished and the
  * device is idle; return the pending asynchronous status (COMPASS_OK or
  * COMPASS_ERR_TIMEOUT) and clear it. COMPASS_ERR_IN_FLIGHT (not cleared) when

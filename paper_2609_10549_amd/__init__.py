@@ -10,6 +10,9 @@ from .compass import (  # noqa: F401
     compass_ag_gemm,
     compass_calibrate,
     compass_decomp_gemm,
+    compass_embed_forward,
+    compass_embed_workspace,
+    compass_embed_backward,
     compass_gemm,
     compass_gemm_rs,
     compass_kernel_times,
@@ -17,6 +20,9 @@ from .compass import (  # noqa: F401
     compass_probe_mfma,
     compass_last_error,
     compass_model_t_comm,
+    compass_norm_forward,
+    compass_norm_workspace,
+    compass_norm_backward,
     compass_partition_layout,
     compass_ring_arrival_times,
     compass_model_t_decomp,
@@ -28,4 +34,8 @@ from .compass import (  # noqa: F401
     compass_sync,
     compass_transfer,
     compass_version,
+    compass_xent_workspace,
+    compass_xent_forward,
+    compass_xent_join,
+    compass_xent_backward,
 )

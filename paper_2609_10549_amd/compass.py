@@ -30,6 +30,9 @@ RING_DOUBLE = 1
 INTRA_FUSION = 0
 INTER_DECOM = 1
 
+BF16 = 0
+F32 = 1
+
 OPT_SPIN_LIMIT = 1
 OPT_HOST_TIMEOUT = 2
 OPT_GRID = 3
@@ -121,6 +124,37 @@ _SIGS = {
                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "compass_transfer": (ctypes.c_int, [ctypes.POINTER(compass_problem), ctypes.POINTER(compass_links), ctypes.c_void_p]),
     "compass_sequential": (ctypes.c_int, [ctypes.POINTER(compass_problem), ctypes.POINTER(compass_links), ctypes.c_void_p]),
+        "compass_xent_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+        "compass_xent_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                          ctypes.c_void_p]),
+        "compass_xent_join": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+        "compass_xent_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                           ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+        "compass_norm_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                          ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+                                          ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                          ctypes.c_void_p, ctypes.c_void_p]),
+        "compass_norm_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+        "compass_norm_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_size_t, ctypes.c_void_p]),
+        "compass_embed_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                           ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+        "compass_embed_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                             ctypes.POINTER(ctypes.c_size_t)]),
+        "compass_embed_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
+                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "compass_sync": (ctypes.c_int, []),
     "compass_kernel_times": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int]),
     "compass_tile_trace": (ctypes.c_int, [ctypes.POINTER(ctypes.c_uint32), ctypes.c_int]),
@@ -346,6 +380,193 @@ def compass_gemm(A, W, C, P=None, stream=None) -> None:
 
 def compass_gemm_noalloc(A, W, C, P=None, stream=None) -> None:
     _gemm_call("compass_gemm_noalloc", A, W, C, P, stream)
+
+
+# ------------------------------------------- the ends of a model (see the header)
+def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False) -> None:
+    """Raise ValueError unless x is a GPU tensor of the given shape whose dtype
+    is one of `kinds` (names), contiguous or, with `rows`, in rows of
+    consecutive elements that do not overlap. Plain int addresses are the
+    caller's responsibility."""
+    if x is None or isinstance(x, int):
+        return
+    if x.shape != shape:
+        raise ValueError(f"{what}: shape {_shape_of(x)}, expected {tuple(shape)}")
+    kind = str(x.dtype)[6:]
+    if kind not in kinds:
+        raise ValueError(f"{what}: {kind}, expected {' or '.join(kinds)}")
+    if not x.is_cuda:
+        raise ValueError(f"{what}: must be on the GPU")
+    if x.is_contiguous():
+        return
+    if not rows or (shape[1] > 1 and x.stride(1) != 1) or (shape[0] > 1 and x.stride(0) < shape[1]):
+        raise ValueError(f"{what}: must be contiguous" + (" within rows" if rows else ""))
+
+
+_BITS = ("bfloat16", "int16")        # bf16 values, as bf16 or as raw patterns
+_ELEMENTS = ("bfloat16", "float32")  # operators of either type
+_FLOAT = ("float32",)
+_INDEX = ("int64",)
+
+
+def _kind(x) -> int:
+    return F32 if x.element_size() == 4 else BF16
+
+
+def _ld(x) -> int:
+    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+
+
+def _ws(x) -> int:
+    if x is None or not x.is_cuda or not x.is_contiguous():
+        raise ValueError("workspace: must be a contiguous GPU tensor")
+    return x.numel() * x.element_size()
+
+
+def compass_xent_workspace(M: int, V: int, K: int, backward: bool = False, piece: int = 0) -> int:
+    """Bytes of the workspace of compass_xent_forward or compass_xent_backward."""
+    out = ctypes.c_size_t()
+    _check(lib().compass_xent_workspace(M, V, K, 1 if backward else 0, piece, ctypes.byref(out)),
+           "compass_xent_workspace")
+    return out.value
+
+
+def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0, stream=None) -> None:
+    """lse, tlogit and loss (M each, fp32; loss may be None) of hidden states H
+    (M x K) and the vocabulary rows W (V x K) from id v0; see the header."""
+    M, K = H.shape
+    V = W.shape[0]
+    _typed(H, "H", (M, K), _BITS)
+    _typed(W, "W", (V, K), _BITS)
+    _typed(target, "target", (M,), _INDEX)
+    _typed(lse, "lse", (M,), _FLOAT)
+    _typed(tlogit, "tlogit", (M,), _FLOAT)
+    _typed(loss, "loss", (M,), _FLOAT)
+    rc = (_lib or lib()).compass_xent_forward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(tlogit),
+                                              _addr(loss), _addr(workspace), _ws(workspace), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_xent_forward")
+
+
+def compass_xent_join(lse_parts, tlogit_parts, target, lse, loss, stream=None) -> None:
+    """lse and loss of the whole vocabulary from the n ranks' shards (n x M)."""
+    n, M = lse_parts.shape
+    _typed(lse_parts, "lse_parts", (n, M), _FLOAT)
+    _typed(tlogit_parts, "tlogit_parts", (n, M), _FLOAT)
+    _typed(target, "target", (M,), _INDEX)
+    _typed(lse, "lse", (M,), _FLOAT)
+    _typed(loss, "loss", (M,), _FLOAT)
+    _check(lib().compass_xent_join(n, M, _addr(lse_parts), _addr(tlogit_parts), _addr(target), _addr(lse), _addr(loss),
+                                   _stream(stream)), "compass_xent_join")
+
+
+def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 0, piece: int = 0,
+                          stream=None) -> None:
+    """Gradients dH (M x K) and dW (V x K) of sum(grad * loss); see the header."""
+    M, K = H.shape
+    V = W.shape[0]
+    _typed(H, "H", (M, K), _BITS)
+    _typed(W, "W", (V, K), _BITS)
+    _typed(target, "target", (M,), _INDEX)
+    _typed(lse, "lse", (M,), _FLOAT)
+    _typed(grad, "grad", (M,), _FLOAT)
+    _typed(dH, "dH", (M, K), _BITS)
+    _typed(dW, "dW", (V, K), _BITS)
+    rc = (_lib or lib()).compass_xent_backward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(grad),
+                                               _addr(dH), _addr(dW), piece, _addr(workspace), _ws(workspace),
+                                               _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_xent_backward")
+
+
+def _params(gamma, beta, N: int) -> int:
+    """Checks the norm's parameters (either may be None) and gives their type."""
+    _typed(gamma, "gamma", (N,), _ELEMENTS)
+    _typed(beta, "beta", (N,), _ELEMENTS)
+    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+        raise ValueError(f"gamma and beta: {gamma.dtype} and {beta.dtype}, expected one type")
+    one = gamma if gamma is not None else beta
+    return F32 if one is None else _kind(one)
+
+
+def compass_norm_forward(x, gamma, beta, y, mean, rstd, eps: float = 1e-5, stream=None) -> None:
+    """Layer norm y (M x N, of x's type) with its statistics mean and rstd (M,
+    fp32); gamma and beta may be None. Rows of x and y may lie apart."""
+    M, N = x.shape
+    _typed(x, "x", (M, N), _ELEMENTS, rows=True)
+    _typed(y, "y", (M, N), (str(x.dtype)[6:],), rows=True)
+    ptype = _params(gamma, beta, N)
+    _typed(mean, "mean", (M,), _FLOAT)
+    _typed(rstd, "rstd", (M,), _FLOAT)
+    rc = (_lib or lib()).compass_norm_forward(M, N, _kind(x), ptype, _addr(x), _ld(x), _addr(gamma), _addr(beta), eps,
+                                              _addr(y), _ld(y), _addr(mean), _addr(rstd), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_norm_forward")
+
+
+def compass_norm_workspace(M: int, N: int) -> int:
+    """Bytes of the workspace of compass_norm_backward."""
+    out = ctypes.c_size_t()
+    _check(lib().compass_norm_workspace(M, N, ctypes.byref(out)), "compass_norm_workspace")
+    return out.value
+
+
+def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None) -> None:
+    """dx (of x's type), dgamma and dbeta (N, fp32; None: not wanted) of
+    compass_norm_forward; gamma may be None."""
+    M, N = x.shape
+    kind = (str(x.dtype)[6:],)
+    _typed(x, "x", (M, N), _ELEMENTS, rows=True)
+    _typed(dy, "dy", (M, N), kind, rows=True)
+    _typed(dx, "dx", (M, N), kind, rows=True)
+    ptype = _params(gamma, None, N)
+    _typed(mean, "mean", (M,), _FLOAT)
+    _typed(rstd, "rstd", (M,), _FLOAT)
+    _typed(dgamma, "dgamma", (N,), _FLOAT)
+    _typed(dbeta, "dbeta", (N,), _FLOAT)
+    rc = (_lib or lib()).compass_norm_backward(M, N, _kind(x), ptype, _addr(dy), _ld(dy), _addr(x), _ld(x), _addr(gamma),
+                                               _addr(mean), _addr(rstd), _addr(dx), _ld(dx), _addr(dgamma),
+                                               _addr(dbeta), _addr(workspace),
+                                               0 if workspace is None else _ws(workspace), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_norm_backward")
+
+
+def compass_embed_forward(ids, table, y, scale: float = 1.0, v0: int = 0, stream=None) -> None:
+    """y[t] = scale * table[ids[t] - v0] (T x K, of the table's type), zeros for
+    ids outside the table's rows."""
+    V, K = table.shape
+    T = ids.shape[0]
+    _typed(ids, "ids", (T,), _INDEX)
+    _typed(table, "table", (V, K), _ELEMENTS, rows=True)
+    _typed(y, "y", (T, K), (str(table.dtype)[6:],), rows=True)
+    rc = (_lib or lib()).compass_embed_forward(T, V, K, _kind(table), _addr(ids), v0, _addr(table), _ld(table), scale,
+                                               _addr(y), _ld(y), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_embed_forward")
+
+
+def compass_embed_workspace(T: int, V: int, K: int) -> int:
+    """Bytes of the workspace of compass_embed_backward."""
+    out = ctypes.c_size_t()
+    _check(lib().compass_embed_workspace(T, V, K, ctypes.byref(out)), "compass_embed_workspace")
+    return out.value
+
+
+def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: int = 0, accumulate: bool = False,
+                           stream=None) -> None:
+    """dtable (V x K) of compass_embed_forward from dy (T x K); with accumulate,
+    added to what dtable holds."""
+    T, K = dy.shape
+    V = dtable.shape[0]
+    _typed(ids, "ids", (T,), _INDEX)
+    _typed(dy, "dy", (T, K), _ELEMENTS, rows=True)
+    _typed(dtable, "dtable", (V, K), _ELEMENTS, rows=True)
+    rc = (_lib or lib()).compass_embed_backward(T, V, K, _kind(dy), _kind(dtable), _addr(ids), v0, _addr(dy), _ld(dy),
+                                                scale, _addr(dtable), _ld(dtable), 1 if accumulate else 0,
+                                                _addr(workspace), _ws(workspace), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_embed_backward")
 
 
 def compass_transfer(problem: Problem, lk: compass_links | None = None, stream=None) -> None:

@@ -38,6 +38,59 @@ int compass_sequential(const compass_problem *p, const compass_links *links, voi
     return op_sequential(p, links, stream);
 }
 
+int compass_xent_workspace(int M, int V, int K, int backward, int piece, size_t *bytes) {
+    return op_xent_workspace(M, V, K, backward, piece, bytes);
+}
+
+int compass_xent_forward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0, float
+                         *lse, float *tlogit, float *loss, void *workspace, size_t workspace_bytes, void *stream) {
+    return op_xent_forward(M, V, K, H, W, target, v0, lse, tlogit, loss, workspace, workspace_bytes, stream);
+}
+
+int compass_xent_join(int n, int M, const float *lse_parts, const float *tlogit_parts, const int64_t *target, float
+                      *lse, float *loss, void *stream) {
+    return op_xent_join(n, M, lse_parts, tlogit_parts, target, lse, loss, stream);
+}
+
+int compass_xent_backward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0, const
+                          float *lse, const float *grad, void *dH, void *dW, int piece, void *workspace, size_t
+                          workspace_bytes, void *stream) {
+    return op_xent_backward(M, V, K, H, W, target, v0, lse, grad, dH, dW, piece, workspace, workspace_bytes,
+                            stream);
+}
+
+int compass_norm_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *gamma, const void
+                         *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd, void *stream) {
+    return op_norm_forward(M, N, dtype, ptype, x, ldx, gamma, beta, eps, y, ldy, mean, rstd, stream);
+}
+
+int compass_norm_workspace(int M, int N, size_t *bytes) {
+    return op_norm_workspace(M, N, bytes);
+}
+
+int compass_norm_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *x, int64_t
+                          ldx, const void *gamma, const float *mean, const float *rstd, void *dx, int64_t lddx, float
+                          *dgamma, float *dbeta, void *workspace, size_t workspace_bytes, void *stream) {
+    return op_norm_backward(M, N, dtype, ptype, dy, lddy, x, ldx, gamma, mean, rstd, dx, lddx, dgamma, dbeta,
+                            workspace, workspace_bytes, stream);
+}
+
+int compass_embed_forward(int T, int V, int K, int dtype, const int64_t *ids, int64_t v0, const void *table, int64_t
+                          ldt, float scale, void *y, int64_t ldy, void *stream) {
+    return op_embed_forward(T, V, K, dtype, ids, v0, table, ldt, scale, y, ldy, stream);
+}
+
+int compass_embed_workspace(int T, int V, int K, size_t *bytes) {
+    return op_embed_workspace(T, V, K, bytes);
+}
+
+int compass_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *ids, int64_t v0, const void *dy,
+                           int64_t ldy, float scale, void *dtable, int64_t ldt, int accumulate, void *workspace,
+                           size_t workspace_bytes, void *stream) {
+    return op_embed_backward(T, V, K, dtype, gtype, ids, v0, dy, ldy, scale, dtable, ldt, accumulate, workspace,
+                             workspace_bytes, stream);
+}
+
 int compass_sync(void) { return op_sync(); }
 
 int compass_set_option(int key, long long value) { return op_set_option(key, value); }

@@ -34,6 +34,8 @@ int hip_error(hipError_t e, const char *what) {
     return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+}  // namespace
+
 // The CU count of the current device, looked up on the first call on it.
 int current_num_cu(int *out) {
     int dev = 0;
@@ -52,8 +54,6 @@ int current_num_cu(int *out) {
     *out = g_num_cu[dev];
     return COMPASS_OK;
 }
-
-}  // namespace
 
 int op_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void *C, const float *P, void *stream) {
     if (M < 1 || N < 1 || K < 1 || K % 8 || N % 8)

@@ -1,0 +1,416 @@
+// Layer norm of a rank's row shard, forward and backward (compass_norm_*).
+//
+//   mean = sum x / N, rstd = 1 / sqrt(sum (x - mean)^2 / N + eps)
+//   xh = (x - mean) rstd, y = xh gamma + beta
+//   a = dy gamma, dx = rstd (a - mean(a) - xh mean(a xh))
+//   dgamma = sum_m dy xh, dbeta = sum_m dy
+//
+// A row is read once and stays in the registers of the threads that share it
+// (a wave, or a workgroup of up to 1024): the mean, then the sum of squared
+// distances from it, both in fp32, then the result. Bound by memory.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "compass.h"
+#include "internal.h"
+#include "rowops.h"
+
+namespace compass {
+
+namespace {
+
+struct NormParams {
+    int M, N;
+    int64_t ldx, ldy, lddy, lddx;   // elements between rows
+    const void *x, *gamma, *beta, *dy;
+    int param_f32;                  // gamma and beta in fp32 (else bf16)
+    float eps;
+    void *y, *dx;
+    float *mean, *rstd;
+    const float *mean_in, *rstd_in;
+    float *part;                    // backward: [grid][2][N] sums of dy xh and dy
+    int want_params;                // whether dgamma or dbeta is wanted
+};
+
+template <class T, int V>
+__device__ __forceinline__ void load_row(const T *row, int i, int N, float (&f)[V]) {
+    if (i < N) {
+        const Pack<T, V> p = *reinterpret_cast<const Pack<T, V> *>(row + i);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = to_f32(p.e[e]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = 0.0f;
+    }
+}
+
+// V parameters from element i, `none` where there is no such vector.
+template <int V>
+__device__ __forceinline__ void load_param(const void *p, int f32, float none, int i, int N, float (&f)[V]) {
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = none;
+    } else if (f32) {
+        load_row<float, V>((const float *)p, i, N, f);
+    } else {
+        load_row<Bf16, V>((const Bf16 *)p, i, N, f);
+    }
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_row(T *row, int i, int N, const float (&f)[V]) {
+    if (i < N) {
+        Pack<T, V> p;
+#pragma unroll
+        for (int e = 0; e < V; ++e) p.e[e] = from_f32<T>(f[e]);
+        *reinterpret_cast<Pack<T, V> *>(row + i) = p;
+    }
+}
+
+// Sum over the TPR threads that share a row, in wave order; `s` holds one
+// value per wave. TPR <= 64: the wave alone, no barrier.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float *s) {
+    x = wave_sum(x);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = s[0];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w) x += s[w];
+    }
+    return x;
+}
+
+// TPR threads per row, ITEMS vectors of V elements each.
+template <class T, int V, int TPR, int ITEMS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(const NormParams p) {
+    constexpr int THREADS = TPR < 256 ? 256 : TPR;
+    __shared__ float s0[THREADS / 64], s1[THREADS / 64];
+    const int t = threadIdx.x % TPR;
+    const int m = (int)blockIdx.x * (THREADS / TPR) + (int)threadIdx.x / TPR;
+    if (TPR == 64 && m >= p.M) return;
+    const T *x = (const T *)p.x + (int64_t)m * p.ldx;
+    float f[ITEMS][V];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        load_row<T, V>(x, (i * TPR + t) * V, p.N, f[i]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum += f[i][e];
+    }
+    const float mean = row_sum<TPR>(sum, s0) / (float)p.N;
+    float sq = 0.0f;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i)
+        if ((i * TPR + t) * V < p.N) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                f[i][e] -= mean;
+                sq += f[i][e] * f[i][e];
+            }
+        }
+    const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s1) / (float)p.N + p.eps);
+    T *y = (T *)p.y + (int64_t)m * p.ldy;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+        float g[V], b[V];
+        load_param<V>(p.gamma, p.param_f32, 1.0f, c, p.N, g);
+        load_param<V>(p.beta, p.param_f32, 0.0f, c, p.N, b);
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[i][e] = f[i][e] * rstd * g[e] + b[e];
+        store_row<T, V>(y, c, p.N, f[i]);
+    }
+    if (t == 0) {
+        p.mean[m] = mean;
+        p.rstd[m] = rstd;
+    }
+}
+
+// Each group of TPR threads takes every gridDim-th row (of its place) and
+// keeps its columns' sums of dy xh and dy in registers to the end.
+template <class T, int V, int TPR, int ITEMS>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_backward_kernel(const NormParams p) {
+    constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR, WAVES = TPR / 64;
+    __shared__ float2 s[2][WAVES > 1 ? WAVES : 1];
+    __shared__ float comb[ROWS > 1 ? ROWS * 64 * V * 2 : 1];
+    const int t = threadIdx.x % TPR, r = threadIdx.x / TPR;
+    float g[ITEMS][V], dg[ITEMS][V], db[ITEMS][V];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        load_param<V>(p.gamma, p.param_f32, 1.0f, (i * TPR + t) * V, p.N, g[i]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dg[i][e] = db[i][e] = 0.0f;
+    }
+    const int step = (int)gridDim.x * ROWS;
+    const float inv = 1.0f / (float)p.N;
+    int par = 0;
+    for (int m = (int)blockIdx.x * ROWS + r; m < p.M; m += step, par ^= 1) {
+        const T *x = (const T *)p.x + (int64_t)m * p.ldx, *dy = (const T *)p.dy + (int64_t)m * p.lddy;
+        float xh[ITEMS][V], d[ITEMS][V];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            load_row<T, V>(x, (i * TPR + t) * V, p.N, xh[i]);
+            load_row<T, V>(dy, (i * TPR + t) * V, p.N, d[i]);
+        }
+        const float mean = p.mean_in[m], rstd = p.rstd_in[m];
+        float c1 = 0.0f, c2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                xh[i][e] = (xh[i][e] - mean) * rstd;   // past the row's end d is 0
+                dg[i][e] += d[i][e] * xh[i][e];
+                db[i][e] += d[i][e];
+                d[i][e] *= g[i][e];
+                c1 += d[i][e];
+                c2 += d[i][e] * xh[i][e];
+            }
+        c1 = wave_sum(c1);
+        c2 = wave_sum(c2);
+        if constexpr (WAVES > 1) {
+            // the two halves of s by turns: a wave writes one again only
+            // behind the next row's barrier, when all have read it
+            if ((threadIdx.x & 63) == 0) s[par][threadIdx.x >> 6] = make_float2(c1, c2);
+            __syncthreads();
+            c1 = s[par][0].x;
+            c2 = s[par][0].y;
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) {
+                c1 += s[par][w].x;
+                c2 += s[par][w].y;
+            }
+        }
+        c1 *= inv;
+        c2 *= inv;
+        T *dx = (T *)p.dx + (int64_t)m * p.lddx;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            float o[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = rstd * (d[i][e] - c1 - xh[i][e] * c2);
+            store_row<T, V>(dx, (i * TPR + t) * V, p.N, o);
+        }
+    }
+    if (!p.want_params) return;
+    float *part = p.part + (size_t)blockIdx.x * 2 * (size_t)p.N;
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        const int c = (i * TPR + t) * V;
+        if constexpr (ROWS > 1) {   // one sum per workgroup, in row order
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                comb[((r * 2 + 0) * V + e) * 64 + t] = dg[i][e];
+                comb[((r * 2 + 1) * V + e) * 64 + t] = db[i][e];
+            }
+            __syncthreads();
+            if (r != 0) continue;
+#pragma unroll
+            for (int q = 1; q < ROWS; ++q)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    dg[i][e] += comb[((q * 2 + 0) * V + e) * 64 + t];
+                    db[i][e] += comb[((q * 2 + 1) * V + e) * 64 + t];
+                }
+        }
+        store_row<float, V>(part, c, p.N, dg[i]);
+        store_row<float, V>(part + p.N, c, p.N, db[i]);
+    }
+}
+
+// dgamma and dbeta from `parts` rows of 2 N sums: 64 columns per workgroup, 16
+// waves that take every 16th row, joined in wave order.
+__global__ __launch_bounds__(1024) void norm_params_kernel(int N, int parts, const float *__restrict__ part,
+                                                           float *dgamma, float *dbeta) {
+    __shared__ float s[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int c = (int)blockIdx.x * 64 + lane;
+    float sum = 0.0f;
+    if (c < 2 * N)
+        for (int i = w; i < parts; i += 16) sum += part[(size_t)i * 2 * (size_t)N + c];
+    s[w][lane] = sum;
+    __syncthreads();
+    if (w != 0 || c >= 2 * N) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) sum += s[i][lane];
+    if (c < N) {
+        if (dgamma) dgamma[c] = sum;
+    } else if (dbeta) {
+        dbeta[c - N] = sum;
+    }
+}
+
+constexpr int kMaxCols = 16384;   // a row's elements in 1024 threads' registers, 16 each
+constexpr int kMaxParts = 1024;
+
+int hip_error(hipError_t e, const char *what) {
+    return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Workgroups of the backward pass: as many as the card holds at once, each
+// with at least 8 rows of its own where there are that many, since every
+// workgroup leaves a row of 2 N sums.
+int backward_groups(int M, int rows) {
+    const int groups = (M + rows - 1) / rows;
+    return std::max(1, std::min(groups, std::min(kMaxParts, std::max(256, M / (8 * rows)))));
+}
+
+struct Launch {
+    const NormParams &p;
+    bool backward;
+    hipStream_t stream;
+    int parts;
+    template <class T, int V, int TPR, int ITEMS>
+    void go() {
+        constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
+        if (backward) {
+            parts = backward_groups(p.M, ROWS);
+            norm_backward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)parts), THREADS, 0, stream>>>(p);
+        } else {
+            norm_forward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)((p.M + ROWS - 1) / ROWS)), THREADS, 0, stream>>>(p);
+        }
+    }
+    // the fewest threads (and vectors each) that hold a row
+    template <class T, int V>
+    void pick() {
+        const int n = (p.N + V - 1) / V;
+        if constexpr (V > 1) {
+            if (n <= 64) go<T, V, 64, 1>();
+            else if (n <= 128) go<T, V, 64, 2>();
+            else if (n <= 256) go<T, V, 256, 1>();
+            else if (n <= 512) go<T, V, 256, 2>();
+            else if (n <= 1024) go<T, V, 512, 2>();
+            else if (n <= 2048) go<T, V, 1024, 2>();
+            else go<T, V, 1024, 4>();
+        } else {
+            if (n <= 256) go<T, V, 64, 4>();
+            else if (n <= 512) go<T, V, 64, 8>();
+            else if (n <= 2048) go<T, V, 256, 8>();
+            else if (n <= 4096) go<T, V, 512, 8>();
+            else if (n <= 8192) go<T, V, 1024, 8>();
+            else go<T, V, 1024, 16>();
+        }
+    }
+};
+
+bool aligned16(const void *p, int64_t ld, size_t size) {
+    return ((uintptr_t)p & 15) == 0 && (size_t)ld * size % 16 == 0;
+}
+
+// 16-byte vectors where every row of every operand starts on 16 bytes and
+// holds whole vectors, single elements otherwise.
+int launch(const NormParams &p, int dtype, bool backward, hipStream_t stream) {
+    const size_t size = dtype == COMPASS_F32 ? 4 : 2;
+    const int64_t v = (int64_t)(16 / size);
+    bool wide = p.N % v == 0 && aligned16(p.x, p.ldx, size) && ((uintptr_t)p.gamma & 15) == 0;
+    if (backward) wide = wide && aligned16(p.dy, p.lddy, size) && aligned16(p.dx, p.lddx, size);
+    else wide = wide && aligned16(p.y, p.ldy, size) && ((uintptr_t)p.beta & 15) == 0;
+    Launch l{p, backward, stream, 0};
+    if (dtype == COMPASS_F32) {
+        if (wide) l.pick<float, 4>();
+        else l.pick<float, 1>();
+    } else {
+        if (wide) l.pick<Bf16, 8>();
+        else l.pick<Bf16, 1>();
+    }
+    return l.parts;
+}
+
+int check(int M, int N, int dtype, int ptype) {
+    if (M < 1 || N < 1) return set_error(COMPASS_ERR_INVALID, "need positive M and N");
+    if ((dtype != COMPASS_BF16 && dtype != COMPASS_F32) || (ptype != COMPASS_BF16 && ptype != COMPASS_F32))
+        return set_error(COMPASS_ERR_INVALID, "unknown element type %d or %d", dtype, ptype);
+    if (N > kMaxCols) return set_error(COMPASS_ERR_UNSUPPORTED, "rows of %d elements, at most %d", N, kMaxCols);
+    return COMPASS_OK;
+}
+
+bool off_element(const void *p, int dtype) { return ((uintptr_t)p & (dtype == COMPASS_F32 ? 3 : 1)) != 0; }
+
+}  // namespace
+
+int op_norm_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *gamma,
+                    const void *beta, float eps, void *y, int64_t ldy, float *mean, float *rstd, void *stream) {
+    int rc = check(M, N, dtype, ptype);
+    if (rc != COMPASS_OK) return rc;
+    if (!x || !y || !mean || !rstd) return set_error(COMPASS_ERR_INVALID, "x, y, mean and rstd are required");
+    if (ldx < N || ldy < N) return set_error(COMPASS_ERR_INVALID, "rows of %d elements overlap", N);
+    if (!(eps >= 0.0f)) return set_error(COMPASS_ERR_INVALID, "eps must not be negative");
+    if (off_element(x, dtype) || off_element(y, dtype) || off_element(gamma, ptype) || off_element(beta, ptype))
+        return set_error(COMPASS_ERR_INVALID, "an operand is not aligned to its elements");
+    int cus;
+    if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
+    NormParams p{};
+    p.M = M;
+    p.N = N;
+    p.ldx = ldx;
+    p.ldy = ldy;
+    p.x = x;
+    p.gamma = gamma;
+    p.beta = beta;
+    p.param_f32 = ptype == COMPASS_F32;
+    p.eps = eps;
+    p.y = y;
+    p.mean = mean;
+    p.rstd = rstd;
+    launch(p, dtype, false, (hipStream_t)stream);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? COMPASS_OK : hip_error(e, "layer norm launch");
+}
+
+int op_norm_workspace(int M, int N, size_t *bytes) {
+    const int rc = check(M, N, COMPASS_BF16, COMPASS_BF16);
+    if (rc != COMPASS_OK) return rc;
+    if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
+    *bytes = (size_t)backward_groups(M, 1) * 2 * (size_t)N * 4;
+    return COMPASS_OK;
+}
+
+int op_norm_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                     const void *gamma, const float *mean, const float *rstd, void *dx, int64_t lddx, float *dgamma,
+                     float *dbeta, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check(M, N, dtype, ptype);
+    if (rc != COMPASS_OK) return rc;
+    if (!dy || !x || !mean || !rstd || !dx)
+        return set_error(COMPASS_ERR_INVALID, "dy, x, mean, rstd and dx are required");
+    if (lddy < N || ldx < N || lddx < N) return set_error(COMPASS_ERR_INVALID, "rows of %d elements overlap", N);
+    if (off_element(dy, dtype) || off_element(x, dtype) || off_element(dx, dtype) || off_element(gamma, ptype))
+        return set_error(COMPASS_ERR_INVALID, "an operand is not aligned to its elements");
+    size_t need = 0;
+    op_norm_workspace(M, N, &need);
+    if (dgamma || dbeta) {
+        if (!ws || ((uintptr_t)ws & 15) || ws_bytes < need)
+            return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes (16-byte aligned), need %zu", ws_bytes, need);
+    }
+    int cus;
+    if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
+    NormParams p{};
+    p.M = M;
+    p.N = N;
+    p.ldx = ldx;
+    p.lddy = lddy;
+    p.lddx = lddx;
+    p.x = x;
+    p.dy = dy;
+    p.gamma = gamma;
+    p.param_f32 = ptype == COMPASS_F32;
+    p.dx = dx;
+    p.mean_in = mean;
+    p.rstd_in = rstd;
+    p.part = (float *)ws;
+    p.want_params = dgamma || dbeta;
+    const int parts = launch(p, dtype, true, (hipStream_t)stream);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return hip_error(e, "layer norm launch");
+    if (p.want_params) {
+        norm_params_kernel<<<dim3((unsigned)((2 * N + 63) / 64)), 1024, 0, (hipStream_t)stream>>>(N, parts, p.part,
+                                                                                               dgamma, dbeta);
+        if ((e = hipGetLastError()) != hipSuccess) return hip_error(e, "weight gradient launch");
+    }
+    return COMPASS_OK;
+}
+
+}  // namespace compass

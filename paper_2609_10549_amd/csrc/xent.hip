@@ -1,0 +1,754 @@
+// Softmax cross entropy of a vocabulary shard straight from hidden states and
+// output weight, and its gradients (compass_xent_*).
+//
+//   z[m][v] = sum_k H[m][k] W[v][k]
+//   lse[m]  = log sum_v exp z[m][v],  loss[m] = lse[m] - z[m][target[m]]
+//   dz[m][v] = grad[m] (exp(z[m][v] - lse[m]) - [v == target[m]])
+//   dH = dz W,  dW = dz^T H
+//
+// The logits never reach memory: forward, each tile of z is reduced to a
+// maximum and a sum of exponentials per row in its epilogue; backward, z is
+// computed again in pieces of the vocabulary and leaves its tile as dz in
+// bf16, which two products then read.
+//
+// tile_kernel is one bf16 MFMA product C = A B over a reduction axis whose
+// operands may each lie with the reduction along their rows (H, W in z = H W^T,
+// dz in dz W) or across them (W in dz W, dz and H in dz^T H). Operands of the
+// second kind go to LDS as they lie, 64 reduction rows of a tile's columns per
+// stage, and reach the matrix cores through the transposing LDS read
+// (ds_read_b64_tr_b16), so no transposed copy of W, H or dz is made.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "compass.h"
+#include "gemm_core.h"
+#include "internal.h"
+#include "kernel_params.h"
+
+namespace compass {
+
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+enum Epilogue : int {
+    kStats = 0,   // row maxima and sums of exponentials, the targets' logits
+    kDz = 1,      // dz in bf16
+    kStore = 2,   // the product: bf16, or fp32 partial sums
+};
+
+struct TileParams {
+    const uint16_t *A, *B;
+    uint64_t a_bytes, b_bytes;   // extents; loads beyond them read zero
+    int M, N, R;                 // rows and columns of C, reduction length
+    int lda, ldb;                // elements between rows of A and B as they lie
+    int tiles_m, tiles_n, group_m;
+    int slices, kslice;          // reduction slices (kslice a multiple of 64)
+    // kStats
+    float2 *parts;               // [2 tiles_n][M]: maximum, sum
+    float *tlogit;
+    // kStats, kDz
+    const int64_t *target;
+    int64_t v0;                  // vocabulary id of column 0
+    // kDz
+    const float *lse, *grad;
+    uint16_t *dz;
+    int ldz;                     // columns [N, ldz) are zero
+    // kStore
+    uint16_t *C;                 // bf16, rows of N (or null)
+    float *part_out;             // fp32 [slices][M][N] (or null)
+    const float *part_in;        // added first, same layout as part_out (or null)
+};
+
+// f(row) of the 16-byte chunk permutation of an operand that lies across the
+// reduction: chunk c of LDS row `row` is at chunk c ^ f. Two neighbouring
+// chunks (16 columns) stay together, and the eight rows that half a wave reads
+// at once fall into eight different 32-byte bank groups (rows of 128 bytes:
+// two rows share a line of banks, four groups each).
+template <int RB>
+__device__ __forceinline__ int cross_swizzle(int row) {
+    return RB >= 256 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
+}
+
+// Loads of one operand's stages: `D` rows (or columns) of the tile, 64 of the
+// reduction per stage. T: the operand lies across the reduction.
+template <bool T, int D>
+struct Loader {
+    static constexpr int L = D / 32;     // loads per wave and stage
+    static constexpr int RB = D * 2;     // bytes of an LDS row (T)
+    uint32_t off[L];
+    i32x4 rsrc;
+    uint64_t base;
+    int64_t left, step;
+    int kc, ke;
+
+    __device__ __forceinline__ void init(const uint16_t *p, uint64_t bytes, int d0, int dim, int ld, int kb, int kend,
+                                         int lane, int wave) {
+        if constexpr (T) {
+            const uint64_t o = ((uint64_t)kb * (uint64_t)ld + (uint64_t)d0) * 2u;
+            base = (uint64_t)p + o;
+            left = (int64_t)bytes - (int64_t)o;
+            step = (int64_t)ld * 128;
+            constexpr int CPR = RB / 16, RPB = 64 / CPR;   // chunks per row, rows per load
+#pragma unroll
+            for (int j = 0; j < L; ++j) {
+                const int row = (j * 4 + wave) * RPB + lane / CPR;
+                const int chunk = (lane % CPR) ^ cross_swizzle<RB>(row);
+                off[j] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)chunk * 16u;
+            }
+        } else {
+            rsrc = tile_rsrc4(p, bytes, (uint64_t)d0 * (uint64_t)ld * 2u);
+            // resource words that came out of vector registers need five wait
+            // states before a load reads them
+            asm volatile("s_nop 4" : "+s"(rsrc));
+            const int lrow0 = 8 * wave + (lane >> 3);
+#pragma unroll
+            for (int q = 0; q < L; ++q) {
+                const int i = 32 * q + lrow0;
+                off[q] = d0 + i < dim ? (uint32_t)i * (uint32_t)ld * 2u : kOOBRow;
+            }
+            kc = kb + ((lane & 7) ^ ((4 * wave + (lane >> 4)) & 7)) * 8;
+            ke = kend;
+        }
+    }
+
+    // The resource of the next stage and the lane's offset in it.
+    __device__ __forceinline__ uint32_t next(i32x4 &r) {
+        if constexpr (T) {
+            const int64_t b = left < 0 ? 0 : left < (int64_t)kTileSpanMax ? left : (int64_t)kTileSpanMax;
+            r[0] = (int)(uint32_t)base;
+            r[1] = (int)((uint32_t)(base >> 32) & 0xFFFFu);
+            r[2] = (int)b;
+            r[3] = 0x00020000;
+            base += (uint64_t)step;
+            left -= step;
+            return 0u;
+        } else {
+            r = rsrc;
+            const uint32_t o = kc < ke ? (uint32_t)kc * 2u : kOOBCol;
+            kc += kBK;
+            return o;
+        }
+    }
+};
+
+// Fragments of one operand out of its LDS stage: F blocks of 16 rows (columns).
+template <bool T, int D, int F>
+struct Reader {
+    static constexpr int RB = D * 2;
+    uint32_t at[T ? F : 2];   // T: lane address of each block; else of each half of the stage
+    __device__ __forceinline__ void init(uint32_t d0, int lane) {
+        const int r = lane & 15, kq = lane >> 4;
+        if constexpr (T) {
+            const int row = kq * 8 + (r >> 2);
+            const uint32_t line = (uint32_t)(row * RB + (r & 1) * 8);
+#pragma unroll
+            for (int f = 0; f < F; ++f) {
+                const int chunk = (((int)d0 / 8 + 2 * f + ((r & 3) >> 1)) ^ cross_swizzle<RB>(row));
+                at[f] = line + (uint32_t)chunk * 16u;
+            }
+        } else {
+            const int swz = (r >> 1) & 7;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) at[s] = (d0 + (uint32_t)r) * 128u + (uint32_t)(((4 * s + kq) ^ swz) << 4);
+        }
+    }
+    // block f of substep S (32 of the reduction) of the stage at LDS offset buf
+    template <int S>
+    __device__ __forceinline__ bf16x8 read(uint32_t buf, int f) const {
+        if constexpr (T) {
+            typedef __attribute__((address_space(3))) s16x4 lds4;
+            const uint32_t a = buf + at[f] + S * 32 * RB;
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)a);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4 *)(uintptr_t)(a + 4 * RB));
+            return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            typedef const __attribute__((address_space(3))) bf16x8 lds8;
+            return *(lds8 *)(uintptr_t)(buf + at[S] + (uint32_t)f * 2048u);
+        }
+    }
+};
+
+// `read` of the fragments whose slot is I.
+template <int F, int NF, int I, int R0, int R1, class Read>
+__device__ __forceinline__ void read_slot(const Read &read) {
+    if constexpr (F < NF) {
+        if constexpr (slot_of(F, NF, R0, R1) == I) read(std::integral_constant<int, F>{});
+        read_slot<F + 1, NF, I, R0, R1>(read);
+    }
+}
+
+// MFMAs [I, I1) of a substep; `read(F)` of the next substep's FM + FN
+// fragments spread over slots [R0, R1), `load(j)` of LC loads over [D0, D1).
+template <int I, int I1, int R0, int R1, int LC, int D0, int D1, int FM, int FN, class Read, class Load>
+__device__ __forceinline__ void mfma_run(f32x4 (&acc)[FN][FM], const bf16x8 (&a)[FM], const bf16x8 (&b)[FN],
+                                         const Read &read, const Load &load) {
+    if constexpr (I < I1) {
+        constexpr int NI = I / FM, MI = slot_row<FM>(I);
+        acc[NI][MI] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[NI], a[MI], acc[NI][MI], 0, 0, 0);
+        read_slot<0, FM + FN, I, R0, R1>(read);
+#pragma unroll
+        for (int j = 0; j < LC; ++j)
+            if (slot_of(j, LC, D0, D1) == I) load(j);
+        __builtin_amdgcn_sched_barrier(0);
+        mfma_run<I + 1, I1, R0, R1, LC, D0, D1, FM, FN>(acc, a, b, read, load);
+    }
+}
+
+__device__ __forceinline__ float wave16_max(float x) {   // over the four lanes of a row
+    x = fmaxf(x, __shfl_xor(x, 16));
+    return fmaxf(x, __shfl_xor(x, 32));
+}
+__device__ __forceinline__ float wave16_sum(float x) {
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+// One BM x BN tile per workgroup; 4 waves, 2 x 2 over the tile. The main loop
+// (stages of 64, DW + 1 buffers of A and DW of B, counted waits, one barrier
+// per stage, LDS reads and loads one at a time between the MFMAs) is
+// gemm_kernel's; see there for what each part of it is worth.
+template <int BM, int BN, int DW, bool AT, bool BT, int EPI>
+__global__ __launch_bounds__(kThreads, (160 << 10) / (((DW + 1) * BM + DW * BN) * 128))
+void tile_kernel(const TileParams p) {
+    constexpr int WM = BM / 2, WN = BN / 2;
+    constexpr int FM = WM / 16, FN = WN / 16;
+    constexpr int LA = BM / 32, LW = BN / 32;
+    constexpr int SA = BM * 128, SW = BN * 128;
+    constexpr int NA = DW + 1;
+    constexpr bool kAcc = NA * SA + DW * SW > (80 << 10);   // one workgroup per CU
+    __shared__ __attribute__((aligned(1024))) char smem[NA * SA + DW * SW];
+
+    const int tid = threadIdx.x;
+    const int lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm0 = (wave >> 1) * WM, wn0 = (wave & 1) * WN;
+
+    // consecutive positions to one XCD (workgroups go round-robin over the 8
+    // XCDs), group_m row tiles before the next column tile: the tiles an XCD
+    // holds at a time share rows of A and columns of B in its L2
+    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.slices;
+    const int v = (int)blockIdx.x & 7, c = (int)blockIdx.x >> 3;
+    const int pos = v * (total >> 3) + min(v, total & 7) + c;
+    const int slice = pos / tiles, tpos = pos - slice * tiles;
+    const int gsz = p.group_m * p.tiles_n;
+    const int grp = tpos / gsz, rin = tpos - grp * gsz;
+    const int rows_here = min(p.group_m, p.tiles_m - grp * p.group_m);
+    const int m0 = (grp * p.group_m + rin % rows_here) * BM;
+    const int n0 = (rin / rows_here) * BN;
+    const int kb = slice * p.kslice, ke = min(p.R, kb + p.kslice);
+
+    f32x4 acc[FN][FM];
+#pragma unroll
+    for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+        for (int mi = 0; mi < FM; ++mi) acc[ni][mi] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    {
+        Loader<AT, BM> la;
+        Loader<BT, BN> lb;
+        la.init(p.A, p.a_bytes, m0, p.M, p.lda, kb, ke, lane, wave);
+        lb.init(p.B, p.b_bytes, n0, p.N, p.ldb, kb, ke, lane, wave);
+        Reader<AT, BM, FM> ra;
+        Reader<BT, BN, FN> rb;
+        ra.init(wm0, lane);
+        rb.init(wn0, lane);
+        const int KT = (ke - kb + kBK - 1) / kBK;
+        const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(smem);
+        const uint32_t ldsW = lds0 + NA * SA, ldsE = ldsW + DW * SW;
+        const uint32_t wb = (uint32_t)wave * 1024u;
+        i32x4 sA, sB;
+#pragma unroll
+        for (int i = 0; i < DW; ++i) {
+            uint32_t o = la.next(sA);
+            load_blocks<LA>(sA, lds0 + i * SA, la.off, o, wave);
+            o = lb.next(sB);
+            load_blocks<LW>(sB, ldsW + i * SW, lb.off, o, wave);
+        }
+        wait_vm_lgkm0<(DW - 1) * (LA + LW)>();
+        lds_barrier();
+        bf16x8 a0[FM], b0[FN], a1[FM], b1[FN];
+#pragma unroll
+        for (int mi = 0; mi < FM; ++mi) a0[mi] = ra.template read<0>(lds0, mi);
+#pragma unroll
+        for (int ni = 0; ni < FN; ++ni) b0[ni] = rb.template read<0>(ldsW, ni);
+        constexpr int NM = FM * FN;
+        constexpr int RE = NM - NM / 4;     // substep 0's reads end here, ahead of the barrier's wait
+        constexpr int B1 = NM / 16;         // MFMAs of substep 1 before the barrier
+        // fragments in the order an MFMA substep needs them: b[0], a[..], b[1..]
+        uint32_t aC = lds0, aF = lds0 + DW * SA, wC = ldsW;
+        if constexpr (kAcc) {
+            // Every accumulator in a register of its own from before the loop,
+            // then around it: from the constant zero the compiler rotates them
+            // (364 to 604 moves per stage and spills).
+#pragma unroll
+            for (int i = 0; i < NM; ++i) asm volatile("" : "+a"(acc[i / FM][slot_row<FM>(i)]));
+        }
+        for (int st = 0; st < KT; ++st) {
+            const uint32_t aN = aC + SA == ldsW ? lds0 : aC + SA, wN = wC + SW == ldsE ? ldsW : wC + SW;
+            if constexpr (kAcc) {   // every accumulator in its own register around the loop
+#pragma unroll
+                for (int i = 0; i < NM; ++i) asm volatile("" : "+a"(acc[i / FM][slot_row<FM>(i)]));
+            }
+            const uint32_t oA = la.next(sA), oB = lb.next(sB);
+            auto read1 = [&](auto fc) __attribute__((always_inline)) {
+                constexpr int f = decltype(fc)::value;
+                if constexpr (f >= 1 && f <= FM) a1[f - 1] = ra.template read<1>(aC, f - 1);
+                else b1[f == 0 ? 0 : f - FM] = rb.template read<1>(wC, f == 0 ? 0 : f - FM);
+            };
+            auto read0 = [&](auto fc) __attribute__((always_inline)) {
+                constexpr int f = decltype(fc)::value;
+                if constexpr (f >= 1 && f <= FM) a0[f - 1] = ra.template read<0>(aN, f - 1);
+                else b0[f == 0 ? 0 : f - FM] = rb.template read<0>(wN, f == 0 ? 0 : f - FM);
+            };
+            auto loadA = [&](int j) { dma16(sA, la.off[j] + oA, aF + wb + (uint32_t)j * 4096u); };
+            auto loadB = [&](int j) { dma16(sB, lb.off[j] + oB, wC + wb + (uint32_t)j * 4096u); };
+            mfma_run<0, NM, 0, RE, LA, 0, NM, FM, FN>(acc, a0, b0, read1, loadA);
+            mfma_run<0, B1, NM, NM + 1, 0, 0, 1, FM, FN>(acc, a1, b1, read0, loadA);
+            wait_vm_lgkm0<(DW - 1) * LA + (DW - 2) * LW>();
+            lds_barrier();
+            mfma_run<B1, NM, B1, NM, LW, B1, B1 + (NM - B1) * 3 / 4, FM, FN>(acc, a1, b1, read0, loadB);
+            aF = aC;
+            aC = aN;
+            wC = wN;
+        }
+        wait_vm_lgkm0<0>();   // the loads past the end land before the buffers are reused
+        __syncthreads();
+    }
+
+    // thread coordinates the compiler cannot see to be known before the main
+    // loop: what is derived from them is computed here, not kept (spilled)
+    // over the loop
+    int et = lane;
+    asm volatile("" : "+v"(et));
+    // lane (er, eq) holds of block (mi, ni): row er, columns 4 eq + 0..3
+    const int er = et & 15, eq = et >> 4;
+    if constexpr (EPI == kStats) {
+        const int c0 = n0 + wn0 + 4 * eq;
+        const bool edge = n0 + BN > p.N;
+        float2 *out = p.parts + (size_t)(2 * (n0 / BN) + (wave & 1)) * (size_t)p.M;
+#pragma unroll
+        for (int mi = 0; mi < FM; ++mi) {
+            const int m = m0 + wm0 + mi * 16 + er;
+            float z[FN][4], mx = -INFINITY;
+#pragma unroll
+            for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z[ni][e] = edge && c0 + ni * 16 + e >= p.N ? -INFINITY : acc[ni][mi][e];
+                    mx = fmaxf(mx, z[ni][e]);
+                }
+            mx = wave16_max(mx);
+            const float sub = mx == -INFINITY ? 0.0f : mx;   // no column of this half is inside
+            float sum = 0.0f;
+#pragma unroll
+            for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[ni][e] - sub) * kLog2e);
+            sum = wave16_sum(sum);
+            if (m < p.M) {
+                if (eq == 0) out[m] = make_float2(mx, sum);
+                const int64_t t = p.target[m] - p.v0 - c0;
+#pragma unroll
+                for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (t == ni * 16 + e && c0 + ni * 16 + e < p.N) p.tlogit[m] = z[ni][e];
+            }
+        }
+    } else {
+        // each wave turns 32 rows at a time to row order through a region of
+        // the freed stage buffers, as gemm_kernel's epilogue does
+        constexpr int CPR = 2 * FN, NIT = 32 * CPR / 64, RB = FN * 64;
+        static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
+        char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
+        auto to_lds = [&](int mi) {
+            char *w = region[mi & 1] + er * RB;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int ni = 0; ni < FN; ++ni)
+                    *reinterpret_cast<f32x4 *>(w + h * 16 * RB + (((4 * ni + eq) ^ (er & 7)) << 4)) = acc[ni][2 * mi + h];
+            asm volatile("" ::: "memory");
+        };
+        to_lds(0);
+#pragma unroll
+        for (int mi = 0; mi < FM / 2; ++mi) {
+            if (mi + 1 < FM / 2) to_lds(mi + 1);
+#pragma unroll
+            for (int it = 0; it < NIT; ++it) {
+                const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
+                const char *w = region[mi & 1] + row * RB;
+                // half of the lanes take their two chunks in the other order,
+                // so that 8 lanes read 8 different bank groups
+                const int sw = (j >> 2) & 1;
+                const f32x4 u0 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + sw) ^ (row & 7)) << 4));
+                const f32x4 u1 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + 1 - sw) ^ (row & 7)) << 4));
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[e] = sw ? u1[e] : u0[e];
+                    x[4 + e] = sw ? u0[e] : u1[e];
+                }
+                const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
+                if constexpr (EPI == kDz) {
+                    if (m < p.M && n < p.ldz) {
+                        const int64_t t0 = p.target[m];
+                        const int64_t t = t0 - p.v0 - n;
+                        const float lse = p.lse[m], g = p.grad[m];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float pr = __builtin_amdgcn_exp2f((x[e] - lse) * kLog2e) - (t == e ? 1.0f : 0.0f);
+                            x[e] = t0 < 0 || n + e >= p.N ? 0.0f : g * pr;
+                        }
+                        *reinterpret_cast<u32x4 *>(p.dz + (size_t)m * (size_t)p.ldz + n) =
+                            u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                  pack_bf16x2(x[6], x[7])};
+                    }
+                } else {
+                    if (m < p.M && n < p.N) {   // N is a multiple of 8
+                        const size_t at = ((size_t)slice * (size_t)p.M + (size_t)m) * (size_t)p.N + n;
+                        if (p.part_in) {
+                            const f32x4 q0 = *reinterpret_cast<const f32x4 *>(p.part_in + at);
+                            const f32x4 q1 = *reinterpret_cast<const f32x4 *>(p.part_in + at + 4);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                x[e] += q0[e];
+                                x[4 + e] += q1[e];
+                            }
+                        }
+                        if (p.part_out) {
+                            *reinterpret_cast<f32x4 *>(p.part_out + at) = f32x4{x[0], x[1], x[2], x[3]};
+                            *reinterpret_cast<f32x4 *>(p.part_out + at + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                        } else {
+                            *reinterpret_cast<u32x4 *>(p.C + (size_t)m * (size_t)p.N + n) =
+                                u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                                      pack_bf16x2(x[6], x[7])};
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Joins a row's parts: lse = max + log sum_i s_i exp(m_i - max). 16 rows per
+// workgroup, 16 lanes each.
+__global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, const float2 *__restrict__ part,
+                                                    const int64_t *target, int64_t v0, float *lse, float *tlogit,
+                                                    float *loss) {
+    __shared__ float2 s_part[16][16];
+    const int r = threadIdx.x & 15, q = threadIdx.x >> 4;
+    const int m = (int)blockIdx.x * 16 + r;
+    float mx = -INFINITY, sum = 0.0f;
+    auto add = [&](float2 x) {
+        const float top = fmaxf(mx, x.x), sub = top == -INFINITY ? 0.0f : top;
+        sum = sum * __builtin_amdgcn_exp2f((mx - sub) * kLog2e) + x.y * __builtin_amdgcn_exp2f((x.x - sub) * kLog2e);
+        mx = top;
+    };
+    if (m < M)
+        for (int i = q; i < parts; i += 16) add(part[(size_t)i * (size_t)M + m]);
+    s_part[q][r] = make_float2(mx, sum);
+    __syncthreads();
+    if (q != 0 || m >= M) return;
+    for (int i = 1; i < 16; ++i) add(s_part[i][r]);
+    const float l = mx + logf(sum);
+    const int64_t t = target[m];
+    float tl = 0.0f;
+    if (t >= v0 && t - v0 < V) tl = tlogit[m];
+    else tlogit[m] = 0.0f;
+    lse[m] = l;
+    if (loss) loss[m] = t < 0 ? 0.0f : l - tl;
+}
+
+// The same over the n ranks' shards of the vocabulary.
+__global__ __launch_bounds__(256) void join_ranks_kernel(int n, int M, const float *__restrict__ lse_parts,
+                                                         const float *__restrict__ tlogit_parts, const int64_t *target,
+                                                         float *lse, float *loss) {
+    const int m = (int)blockIdx.x * 256 + (int)threadIdx.x;
+    if (m >= M) return;
+    float mx = -INFINITY;
+    for (int q = 0; q < n; ++q) mx = fmaxf(mx, lse_parts[(size_t)q * (size_t)M + m]);
+    const float sub = mx == -INFINITY ? 0.0f : mx;
+    float sum = 0.0f, tl = 0.0f;
+    for (int q = 0; q < n; ++q) {
+        sum += __builtin_amdgcn_exp2f((lse_parts[(size_t)q * (size_t)M + m] - sub) * kLog2e);
+        tl += tlogit_parts[(size_t)q * (size_t)M + m];
+    }
+    const float l = sub + logf(sum);
+    lse[m] = l;
+    loss[m] = target[m] < 0 ? 0.0f : l - tl;
+}
+
+// out = bf16(sum of the slices in order), 4 values per thread.
+__global__ __launch_bounds__(256) void join_slices_kernel(size_t count4, int slices, const f32x4 *__restrict__ part,
+                                                          uint16_t *out) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count4) return;
+    f32x4 x = part[i];
+    for (int s = 1; s < slices; ++s) x += part[(size_t)s * count4 + i];
+    *reinterpret_cast<u32x2 *>(out + 4 * i) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+}
+
+// ------------------------------------------------------------------- plans
+
+struct Shape { int rows, cols, wg_per_cu; double stage_us, edge_us; };
+constexpr Shape kShapes[] = {
+    {256, 256, 1, 1.40, 9.0}, {128, 128, 2, 0.90, 5.0}, {64, 64, 2, 0.45, 3.0}};
+constexpr int kShapeCount = 3;
+constexpr int kCUs = 256;   // the card this library is built for; sizes of workspaces follow from it
+
+struct TilePlan { int shape, tiles_m, tiles_n, slices, kslice; };
+
+// The cheapest tile (and slices of the reduction, at most max_slices) by
+// rounds of workgroups times a tile's time.
+TilePlan plan_tiles(int M, int N, int R, int max_slices) {
+    TilePlan best{};
+    double best_t = 0;
+    for (int s = 0; s < kShapeCount; ++s) {
+        const Shape &sh = kShapes[s];
+        const int tm = (M + sh.rows - 1) / sh.rows, tn = (N + sh.cols - 1) / sh.cols;
+        const double tiles = (double)tm * tn;
+        const int stages = (R + kBK - 1) / kBK;
+        for (int k = 1; k <= max_slices && (k == 1 || stages / k >= 8); ++k) {
+            const int per = (stages + k - 1) / k;
+            const int ns = (stages + per - 1) / per;
+            const double rounds = std::max(1.0, tiles * ns / (kCUs * sh.wg_per_cu));
+            const double whole = rounds < 4 ? (double)(int64_t)(rounds + 0.999) : rounds + 0.5;
+            double t = whole * (per * sh.stage_us + sh.edge_us);
+            if (ns > 1) t += 5.0 + 8.0e-6 * (double)M * N * ns / 4.0;   // fp32 slices out and in
+            if (best_t == 0 || t < best_t) {
+                best_t = t;
+                best = {s, tm, tn, ns, per * kBK};
+            }
+        }
+    }
+    return best;
+}
+
+template <bool AT, bool BT, int EPI>
+hipError_t launch_tiles(TileParams &p, const TilePlan &pl, hipStream_t stream) {
+    p.tiles_m = pl.tiles_m;
+    p.tiles_n = pl.tiles_n;
+    p.slices = pl.slices;
+    p.kslice = pl.kslice;
+    p.group_m = pl.shape == 0 ? 4 : 8;
+    const dim3 grid((unsigned)(pl.tiles_m * pl.tiles_n * pl.slices));
+    switch (pl.shape) {
+    case 0: tile_kernel<256, 256, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 1: tile_kernel<128, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    default: tile_kernel<64, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    }
+    return hipGetLastError();
+}
+
+int hip_error(hipError_t e, const char *what) {
+    return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+constexpr int kMaxSlices = 16;
+constexpr size_t kPieceBytes = (size_t)512 << 20;   // dz of a default piece
+
+// Pieces of the vocabulary of a backward pass, all but the last `cols` wide.
+struct Pieces { int cols, count; };
+Pieces plan_pieces(int M, int V, int piece) {
+    int cols = piece;
+    if (cols == 0) {
+        const size_t fit = std::max<size_t>(kPieceBytes / ((size_t)M * 2) / 256 * 256, 256);
+        if ((size_t)V <= fit) cols = V;
+        else {
+            const int count = (int)((V + fit - 1) / fit);
+            cols = ((V + count - 1) / count + 255) / 256 * 256;
+        }
+    }
+    cols = std::min(cols, V);
+    return {cols, (V + cols - 1) / cols};
+}
+
+int dz_columns(int cols) { return (cols + 63) / 64 * 64; }
+
+struct BackwardPlan {
+    Pieces pieces;
+    TilePlan dh;      // of a whole piece
+    int ldz;
+    size_t dz_bytes, part_bytes;
+};
+BackwardPlan plan_backward(int M, int V, int K, int piece) {
+    BackwardPlan b;
+    b.pieces = plan_pieces(M, V, piece);
+    b.ldz = dz_columns(b.pieces.cols);
+    b.dh = plan_tiles(M, K, b.ldz, kMaxSlices);
+    b.dz_bytes = align256((size_t)M * (size_t)b.ldz * 2);
+    b.part_bytes = b.pieces.count > 1 || b.dh.slices > 1 ? (size_t)b.dh.slices * (size_t)M * (size_t)K * 4 : 0;
+    return b;
+}
+
+size_t forward_bytes(int M, int V, int K) {
+    return (size_t)plan_tiles(M, V, K, 1).tiles_n * 2 * (size_t)M * sizeof(float2);
+}
+
+constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxDepth = 1 << 17;
+
+int check_sizes(int M, int V, int K) {
+    if (M < 1 || V < 1 || K < 1 || K % 8)
+        return set_error(COMPASS_ERR_INVALID, "need positive M, V and K with K a multiple of 8");
+    if (M > kMaxRows || V > kMaxVocab || K > kMaxDepth)
+        return set_error(COMPASS_ERR_UNSUPPORTED, "M = %d, V = %d, K = %d beyond %d, %d, %d", M, V, K, kMaxRows,
+                         kMaxVocab, kMaxDepth);
+    return COMPASS_OK;
+}
+
+bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
+
+}  // namespace
+
+int op_xent_workspace(int M, int V, int K, int backward, int piece, size_t *bytes) {
+    const int rc = check_sizes(M, V, K);
+    if (rc != COMPASS_OK) return rc;
+    if (!bytes || piece < 0) return set_error(COMPASS_ERR_INVALID, "bytes is required, piece must not be negative");
+    if (backward) {
+        const BackwardPlan b = plan_backward(M, V, K, piece);
+        *bytes = b.dz_bytes + b.part_bytes;
+    } else {
+        *bytes = forward_bytes(M, V, K);
+    }
+    return COMPASS_OK;
+}
+
+int op_xent_forward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0, float *lse,
+                    float *tlogit, float *loss, void *ws, size_t ws_bytes, void *stream) {
+    int rc = check_sizes(M, V, K);
+    if (rc != COMPASS_OK) return rc;
+    if (!H || !W || !target || !lse || !tlogit || !ws)
+        return set_error(COMPASS_ERR_INVALID, "H, W, target, lse, tlogit and the workspace are required");
+    if (misaligned(H) || misaligned(W) || misaligned(ws))
+        return set_error(COMPASS_ERR_INVALID, "H, W and the workspace must be 16-byte aligned");
+    if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
+    const TilePlan pl = plan_tiles(M, V, K, 1);
+    if (ws_bytes < forward_bytes(M, V, K))
+        return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, forward_bytes(M, V, K));
+    int cus;
+    if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
+    TileParams p{};
+    p.A = (const uint16_t *)H;
+    p.B = (const uint16_t *)W;
+    p.a_bytes = (uint64_t)M * (uint64_t)K * 2;
+    p.b_bytes = (uint64_t)V * (uint64_t)K * 2;
+    p.M = M;
+    p.N = V;
+    p.R = p.lda = p.ldb = K;
+    p.parts = (float2 *)ws;
+    p.tlogit = tlogit;
+    p.target = target;
+    p.v0 = v0;
+    hipError_t e = launch_tiles<false, false, kStats>(p, pl, (hipStream_t)stream);
+    if (e != hipSuccess) return hip_error(e, "logits launch");
+    stats_kernel<<<dim3((unsigned)((M + 15) / 16)), 256, 0, (hipStream_t)stream>>>(M, V, 2 * pl.tiles_n, p.parts, target,
+                                                                                v0, lse, tlogit, loss);
+    e = hipGetLastError();
+    return e == hipSuccess ? COMPASS_OK : hip_error(e, "statistics launch");
+}
+
+int op_xent_join(int n, int M, const float *lse_parts, const float *tlogit_parts, const int64_t *target, float *lse,
+                 float *loss, void *stream) {
+    if (n < 1 || M < 1) return set_error(COMPASS_ERR_INVALID, "need positive n and M");
+    if (!lse_parts || !tlogit_parts || !target || !lse || !loss)
+        return set_error(COMPASS_ERR_INVALID, "every operand is required");
+    int cus;
+    const int rc = current_num_cu(&cus);
+    if (rc != COMPASS_OK) return rc;
+    join_ranks_kernel<<<dim3((unsigned)((M + 255) / 256)), 256, 0, (hipStream_t)stream>>>(n, M, lse_parts, tlogit_parts,
+                                                                                       target, lse, loss);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? COMPASS_OK : hip_error(e, "join launch");
+}
+
+int op_xent_backward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0,
+                     const float *lse, const float *grad, void *dH, void *dW, int piece, void *ws, size_t ws_bytes,
+                     void *stream) {
+    int rc = check_sizes(M, V, K);
+    if (rc != COMPASS_OK) return rc;
+    if (!H || !W || !target || !lse || !grad || !dH || !dW || !ws)
+        return set_error(COMPASS_ERR_INVALID, "every operand and the workspace are required");
+    if (misaligned(H) || misaligned(W) || misaligned(dH) || misaligned(dW) || misaligned(ws))
+        return set_error(COMPASS_ERR_INVALID, "H, W, dH, dW and the workspace must be 16-byte aligned");
+    if (v0 < 0 || piece < 0) return set_error(COMPASS_ERR_INVALID, "v0 and piece must not be negative");
+    const BackwardPlan b = plan_backward(M, V, K, piece);
+    if (ws_bytes < b.dz_bytes + b.part_bytes)
+        return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, b.dz_bytes + b.part_bytes);
+    int cus;
+    if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
+    const hipStream_t s = (hipStream_t)stream;
+    uint16_t *dz = (uint16_t *)ws;
+    float *part = (float *)((char *)ws + b.dz_bytes);
+    const uint64_t h_bytes = (uint64_t)M * (uint64_t)K * 2;
+    for (int i = 0; i < b.pieces.count; ++i) {
+        const int c0 = i * b.pieces.cols, cols = std::min(b.pieces.cols, V - c0);
+        const uint16_t *Wp = (const uint16_t *)W + (size_t)c0 * (size_t)K;
+        const uint64_t w_bytes = (uint64_t)cols * (uint64_t)K * 2;
+        TileParams p{};
+        p.A = (const uint16_t *)H;
+        p.B = Wp;
+        p.a_bytes = h_bytes;
+        p.b_bytes = w_bytes;
+        p.M = M;
+        p.N = cols;
+        p.R = p.lda = p.ldb = K;
+        p.target = target;
+        p.v0 = v0 + c0;
+        p.lse = lse;
+        p.grad = grad;
+        p.dz = dz;
+        p.ldz = dz_columns(cols);
+        hipError_t e = launch_tiles<false, false, kDz>(p, plan_tiles(M, p.ldz, K, 1), s);
+        if (e != hipSuccess) return hip_error(e, "dz launch");
+
+        TileParams q{};
+        q.A = dz;
+        q.a_bytes = (uint64_t)M * (uint64_t)p.ldz * 2;
+        q.lda = p.ldz;
+        // dW's rows of this piece = dz^T H
+        q.B = (const uint16_t *)H;
+        q.b_bytes = h_bytes;
+        q.M = cols;
+        q.N = q.ldb = K;
+        q.R = M;
+        q.C = (uint16_t *)dW + (size_t)c0 * (size_t)K;
+        e = launch_tiles<true, true, kStore>(q, plan_tiles(cols, K, M, 1), s);
+        if (e != hipSuccess) return hip_error(e, "dW launch");
+        // dH += dz W over this piece
+        q.B = Wp;
+        q.b_bytes = w_bytes;
+        q.M = M;
+        q.R = p.ldz;
+        q.C = (uint16_t *)dH;
+        q.part_in = i > 0 ? part : nullptr;
+        // the last piece of an unsplit sum leaves rounded
+        q.part_out = b.dh.slices > 1 || i + 1 < b.pieces.count ? part : nullptr;
+        // (a narrower last piece keeps the slice count, so that it adds to the
+        // same partial sums; slices that start past its end add nothing)
+        TilePlan pl = b.dh;
+        const int stages = p.ldz / kBK;
+        pl.kslice = (stages + pl.slices - 1) / pl.slices * kBK;
+        e = launch_tiles<false, true, kStore>(q, pl, s);
+        if (e != hipSuccess) return hip_error(e, "dH launch");
+    }
+    if (b.dh.slices > 1) {
+        const size_t count4 = (size_t)M * (size_t)K / 4;
+        join_slices_kernel<<<dim3((unsigned)((count4 + 255) / 256)), 256, 0, s>>>(count4, b.dh.slices, (const f32x4 *)part,
+                                                                               (uint16_t *)dH);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return hip_error(e, "dH join launch");
+    }
+    return COMPASS_OK;
+}
+
+}  // namespace compass

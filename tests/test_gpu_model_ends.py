@@ -1,0 +1,483 @@
+"""The operators at a model's ends on the GPU (vocabulary cross entropy, layer
+norm, embedding, forward and backward) through the public binding, against the
+fp64 oracle, element by element. The bounds follow from the arithmetic: u8 =
+2^-8, one bf16 rounding; u24 = 2^-24, one fp32 rounding; sums of n terms are
+off by at most n u24 times the sum of their magnitudes."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+
+from oracle import model_ends as E
+from paper_2609_10549_amd import compass as C
+
+pytestmark = pytest.mark.gpu
+
+U8, U24 = 2.0 ** -8, 2.0 ** -24
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _gen(seed):
+    torch = _torch()
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return lambda *s: torch.randn(*s, generator=g, device="cuda")
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _nan(*shape, dtype=None):
+    torch = _torch()
+    return torch.full(shape, float("nan"), dtype=dtype or torch.float32, device="cuda")
+
+
+def _scratch(n):
+    torch = _torch()
+    return torch.full((max(n, 16),), 0xFF, dtype=torch.uint8, device="cuda")   # NaN patterns
+
+
+def _within(name, got, ref, tol):
+    got = _np(got)
+    assert np.isfinite(got).all(), f"{name}: {np.count_nonzero(~np.isfinite(got))} values are not finite"
+    over = np.abs(got - ref) - tol
+    assert (over <= 0).all(), f"{name}: {np.count_nonzero(over > 0)} of {got.size} out of bound, by up to {over.max():.3g}"
+
+
+# ---------------------------------------------------------------- cross entropy
+# from one element to several tiles of every shape; edges inside tiles, stages
+# and 16-byte pieces; few rows against a long vocabulary and the reverse
+XENT = [(1, 1, 8), (1, 1000, 64), (3, 63, 72), (16, 65, 8), (64, 64, 64), (65, 257, 136), (130, 1031, 520),
+        (257, 4099, 264), (8, 9001, 1032), (777, 3001, 1544), (1024, 1536, 256), (2100, 130, 328), (520, 20011, 512)]
+
+
+def _xent_inputs(M, V, K, seed, span=None, lean=6.0):
+    """span: ids of the whole vocabulary (default: the shard's)."""
+    torch = _torch()
+    n = _gen(seed)
+    W = (n(V, K) * (1.5 / K ** 0.5)).bfloat16()
+    target = torch.randint(0, span or V, (M,), generator=torch.Generator().manual_seed(seed)).cuda()
+    H = n(M, K)
+    H = (H + lean / 2.25 * W.float()[target % V]).bfloat16()
+    target[::7] = -100
+    return H, W, target
+
+
+def _xent_tol(H, W):
+    """Per row: what fp32 leaves of a logit and of the log-sum-exp."""
+    M, K = H.shape
+    mag = (np.abs(_np(H)) @ np.abs(_np(W)).T).max(axis=1)
+    z = 2 * K * U24 * mag
+    return z, z + 2 * U24 * (W.shape[0] + 64 + 4 * mag)
+
+
+@pytest.mark.parametrize("M,V,K", XENT)
+def test_xent_forward(M, V, K):
+    print(f"xent forward {M} {V} {K}", flush=True)
+    H, W, t = _xent_inputs(M, V, K, 1)
+    lse, tl, loss = _nan(M), _nan(M), _nan(M)
+    C.compass_xent_forward(H, W, t, lse, tl, loss, _scratch(C.compass_xent_workspace(M, V, K)))
+    r_lse, r_tl, r_loss = E.xent_forward(_np(H), _np(W), t.cpu().numpy())
+    z, tol = _xent_tol(H, W)
+    _within("lse", lse, r_lse, tol)
+    _within("tlogit", tl, r_tl, z + 2 * U24 * np.abs(r_tl))
+    _within("loss", loss, r_loss, z + tol + 2 * U24 * np.abs(r_loss))
+
+
+def _dz_error(H, W, t, lse, grad, v0):
+    """Bound on the error of each dz element: the exponent's, the subtraction's
+    and the bf16 rounding's."""
+    dz = E.xent_dz(_np(H), _np(W), t.cpu().numpy(), _np(lse), _np(grad), v0)
+    z, tol = _xent_tol(H, W)
+    g = np.abs(_np(grad))[:, None]
+    p = np.exp(E.logits(_np(H), _np(W)) - _np(lse)[:, None])
+    delta = (z + tol + 128 * U24)[:, None] * 1.01
+    return dz, np.abs(dz) * U8 + (1 + U8) * (g * p * delta + np.abs(dz) * 4 * U24 + g * 4 * U24 * (dz != 0))
+
+
+def _check_backward(H, W, t, lse, grad, dH, dW, v0=0):
+    dz, err = _dz_error(H, W, t, lse, grad, v0)
+    h, w = _np(H), _np(W)
+    r_dH, r_dW = dz @ w, dz.T @ h
+    eH = err @ np.abs(w) + 2 * dz.shape[1] * U24 * (np.abs(dz) @ np.abs(w))
+    eW = err.T @ np.abs(h) + 2 * dz.shape[0] * U24 * (np.abs(dz).T @ np.abs(h))
+    _within("dH", dH, r_dH, eH + U8 * (np.abs(r_dH) + eH))
+    _within("dW", dW, r_dW, eW + U8 * (np.abs(r_dW) + eW))
+
+
+def _backward(H, W, t, lse, grad, piece=0, v0=0):
+    torch = _torch()
+    (M, K), V = H.shape, W.shape[0]
+    dH, dW = _nan(M, K, dtype=torch.bfloat16), _nan(V, K, dtype=torch.bfloat16)
+    C.compass_xent_backward(H, W, t, lse, grad, dH, dW,
+                            _scratch(C.compass_xent_workspace(M, V, K, backward=True, piece=piece)), v0=v0, piece=piece)
+    return dH, dW
+
+
+@pytest.mark.parametrize("M,V,K", XENT)
+def test_xent_backward(M, V, K):
+    print(f"xent backward {M} {V} {K}", flush=True)
+    H, W, t = _xent_inputs(M, V, K, 2)
+    lse = _torch().from_numpy(E.xent_forward(_np(H), _np(W), t.cpu().numpy())[0]).float().cuda()
+    grad = (_gen(3)(M) * 0.3 + 1.0) / M
+    _check_backward(H, W, t, lse, grad, *_backward(H, W, t, lse, grad))
+
+
+@pytest.mark.parametrize("M,V,K,piece", [(130, 1031, 520, 256), (257, 4099, 264, 1000), (777, 3001, 1544, 64),
+                                         (8, 9001, 1032, 4500), (1100, 2600, 512, 1300), (5, 100, 64, 1)])
+def test_xent_backward_in_pieces_of_the_vocabulary(M, V, K, piece):
+    print(f"xent backward {M} {V} {K} piece {piece}", flush=True)
+    H, W, t = _xent_inputs(M, V, K, 4)
+    lse = _torch().from_numpy(E.xent_forward(_np(H), _np(W), t.cpu().numpy())[0]).float().cuda()
+    grad = (_gen(5)(M) * 0.3 + 1.0) / M
+    _check_backward(H, W, t, lse, grad, *_backward(H, W, t, lse, grad, piece=piece))
+
+
+@pytest.mark.parametrize("n,M,V,K", [(2, 130, 501, 264), (4, 70, 1000, 136), (8, 33, 77, 64)])
+def test_xent_over_the_ranks_of_a_split_vocabulary(n, M, V, K):
+    """n shards, joined, against the whole vocabulary; the shards' dH add up."""
+    torch = _torch()
+    H, W, t = _xent_inputs(M, n * V, K, 6)
+    lse_p, tl_p = _nan(n, M), _nan(n, M)
+    for q in range(n):
+        C.compass_xent_forward(H, W[q * V:(q + 1) * V], t, lse_p[q], tl_p[q], None,
+                               _scratch(C.compass_xent_workspace(M, V, K)), v0=q * V)
+    lse, loss = _nan(M), _nan(M)
+    C.compass_xent_join(lse_p, tl_p, t, lse, loss)
+    r_lse, _, r_loss = E.xent_forward(_np(H), _np(W), t.cpu().numpy())
+    z, tol = _xent_tol(H, W)
+    _within("lse", lse, r_lse, tol + 2 * U24 * (n + 64 + np.abs(r_lse)))
+    _within("loss", loss, r_loss, z + tol + 2 * U24 * (n + 64 + np.abs(r_lse) + np.abs(r_loss)))
+    grad = torch.full((M,), 1.0 / M, device="cuda")
+    for q in range(n):
+        Wq = W[q * V:(q + 1) * V]
+        dH, dW = _backward(H, Wq, t, lse, grad, v0=q * V)
+        _check_backward(H, Wq, t, lse, grad, dH, dW, v0=q * V)
+
+
+def test_xent_rows_without_a_target_carry_nothing():
+    torch = _torch()
+    M, V, K = 70, 300, 136
+    H, W, t = _xent_inputs(M, V, K, 7)
+    t.fill_(-1)
+    lse, tl, loss = _nan(M), _nan(M), _nan(M)
+    C.compass_xent_forward(H, W, t, lse, tl, loss, _scratch(C.compass_xent_workspace(M, V, K)))
+    assert torch.equal(loss, torch.zeros_like(loss)) and torch.equal(tl, torch.zeros_like(tl))
+    dH, dW = _backward(H, W, t, lse, torch.ones(M, device="cuda"))
+    assert not dH.any() and not dW.any()
+
+
+def test_xent_one_row_of_extreme_logits():
+    """Logits of +-3e4: probabilities underflow to 0 and 1 and stay finite."""
+    torch = _torch()
+    M, V, K = 4, 130, 64
+    W = torch.zeros(V, K, device="cuda").bfloat16()
+    W[:, 0] = torch.linspace(-1, 1, V, device="cuda").bfloat16()
+    H = torch.zeros(M, K, device="cuda").bfloat16()
+    H[:, 0] = torch.tensor([30000.0, -30000.0, 1.0, 0.0], device="cuda").bfloat16()
+    t = torch.tensor([V - 1, V - 1, 3, 5], device="cuda")
+    lse, tl, loss = _nan(M), _nan(M), _nan(M)
+    C.compass_xent_forward(H, W, t, lse, tl, loss, _scratch(C.compass_xent_workspace(M, V, K)))
+    ref = E.xent_forward(_np(H), _np(W), t.cpu().numpy())
+    for name, got, want in zip(("lse", "tlogit", "loss"), (lse, tl, loss), ref):
+        _within(name, got, want, 1e-6 * (np.abs(want) + 3e4 * (np.abs(_np(H)[:, 0]) > 2) + 1))
+    dH, dW = _backward(H, W, t, lse, torch.ones(M, device="cuda"))
+    _check_backward(H, W, t, lse, torch.ones(M, device="cuda"), dH, dW)
+
+
+def test_xent_gradient_against_differences():
+    """<dH, D> and <dW, D> against central differences of the fp64 loss."""
+    torch = _torch()
+    M, V, K = 40, 500, 136
+    H, W, t = _xent_inputs(M, V, K, 8)
+    h, w, tt = _np(H), _np(W), t.cpu().numpy()
+    grad = torch.full((M,), 1.0 / M, device="cuda")
+    lse = torch.from_numpy(E.xent_forward(h, w, tt)[0]).float().cuda()
+    dH, dW = _backward(H, W, t, lse, grad)
+    rng = np.random.default_rng(9)
+    f = lambda a, b: E.xent_forward(a, b, tt)[2].mean()  # noqa: E731
+    for _ in range(4):
+        DH, DW = rng.standard_normal(h.shape), rng.standard_normal(w.shape)
+        e = 1e-4
+        dif = (f(h + e * DH, w) - f(h - e * DH, w)) / (2 * e)
+        # dz and dH are rounded to bf16, independently per element
+        assert abs((_np(dH) * DH).sum() - dif) < 2 * U8 * np.linalg.norm(_np(dH) * DH) + 1e-6
+        dif = (f(h, w + e * DW) - f(h, w - e * DW)) / (2 * e)
+        assert abs((_np(dW) * DW).sum() - dif) < 2 * U8 * np.linalg.norm(_np(dW) * DW) + 1e-6
+
+
+# ------------------------------------------------------------------ layer norm
+# both vector widths, every count of threads per row, odd lengths, one element
+NORM = [(1, 1), (1, 64), (2, 63), (5, 512), (3, 513), (7, 1024), (66, 1032), (4, 2048), (9, 4097), (6, 8192), (5, 12288),
+        (3, 16384), (2, 16383), (300, 96), (1500, 40), (600, 2056)]
+TYPES = [("bfloat16", "bfloat16"), ("float32", "float32"), ("bfloat16", "float32"), ("float32", "bfloat16")]
+_DEPTH = 128   # additions one after another in a row's sums (64 per thread, then the tree)
+
+
+def _norm_inputs(M, N, dtype, ptype, seed, pad=0):
+    torch = _torch()
+    n = _gen(seed)
+    dt, pt = getattr(torch, dtype), getattr(torch, ptype)
+    x = (n(M, N + pad) * (0.5 + torch.rand(M, 1, device="cuda")) + 0.3).to(dt)[:, :N]
+    return x, (1 + 0.2 * n(N)).to(pt), (0.2 * n(N)).to(pt), dt
+
+
+def _unit(dt):
+    return U8 if "bf" in str(dt) else U24
+
+
+def _norm_tol(x, g, mean, rstd, ref):
+    """(mean's, rstd's relative, xh's) errors of the forward pass."""
+    d_mean = _DEPTH * U24 * np.abs(x).mean(axis=1) + U24 * np.abs(mean)
+    d = (d_mean + U24 * np.abs(x).max(axis=1)) * rstd
+    rel = 2 * _DEPTH * U24 + 2 * d
+    xh = np.abs(x - mean[:, None]) * rstd[:, None]
+    return d_mean, rel, d[:, None] + xh * (rel[:, None] + 4 * U24)
+
+
+@pytest.mark.parametrize("dtype,ptype", TYPES)
+@pytest.mark.parametrize("M,N", NORM)
+def test_norm_forward(M, N, dtype, ptype):
+    print(f"norm forward {M} {N} {dtype} {ptype}", flush=True)
+    x, g, b, dt = _norm_inputs(M, N, dtype, ptype, 11)
+    y, mean, rstd = _nan(M, N, dtype=dt), _nan(M), _nan(M)
+    C.compass_norm_forward(x, g, b, y, mean, rstd, eps=1e-5)
+    ry, rm, rr = E.norm_forward(_np(x), _np(g), _np(b), float(np.float32(1e-5)))
+    d_mean, rel, d_xh = _norm_tol(_np(x), _np(g), rm, rr, ry)
+    _within("mean", mean, rm, d_mean)
+    _within("rstd", rstd, rr, rr * rel)
+    e = np.abs(_np(g)) * d_xh + 4 * U24 * (np.abs(ry) + np.abs(_np(b)))
+    _within("y", y, ry, e + _unit(dt) * (np.abs(ry) + e))
+
+
+@pytest.mark.parametrize("dtype,ptype", TYPES)
+@pytest.mark.parametrize("M,N", NORM)
+def test_norm_backward(M, N, dtype, ptype):
+    print(f"norm backward {M} {N} {dtype} {ptype}", flush=True)
+    torch = _torch()
+    x, g, b, dt = _norm_inputs(M, N, dtype, ptype, 12)
+    dy = (_gen(13)(M, N) * 0.01).to(dt)
+    _, rm, rr = E.norm_forward(_np(x), None, None, 1e-5)
+    mean, rstd = torch.from_numpy(rm).float().cuda(), torch.from_numpy(rr).float().cuda()
+    dx, dg, db = _nan(M, N, dtype=dt), _nan(N), _nan(N)
+    C.compass_norm_backward(dy, x, g, mean, rstd, dx, dg, db, _scratch(C.compass_norm_workspace(M, N)))
+    _check_norm_backward(dy, x, g, mean, rstd, dx, dg, db, dt)
+
+
+def _check_norm_backward(dy, x, g, mean, rstd, dx, dg, db, dt):
+    X, D, m, r = _np(x), _np(dy), _np(mean)[:, None], _np(rstd)[:, None]
+    G = np.ones(X.shape[1]) if g is None else _np(g)
+    rdx, rdg, rdb = E.norm_backward(D, X, None if g is None else G, m[:, 0], r[:, 0])
+    xh = (X - m) * r
+    d_xh = 4 * U24 * np.abs(xh) + U24 * (np.abs(X) + np.abs(m)) * r
+    a = np.abs(D * G)
+    d_c1 = (_DEPTH + 4) * U24 * a.mean(axis=1, keepdims=True)
+    d_c2 = (_DEPTH + 4) * U24 * (a * np.abs(xh)).mean(axis=1, keepdims=True) + (a * d_xh).mean(axis=1, keepdims=True)
+    c2 = np.abs((D * G * xh).mean(axis=1, keepdims=True))
+    c1 = np.abs((D * G).mean(axis=1, keepdims=True))
+    e = r * (d_c1 + np.abs(xh) * d_c2 + d_xh * c2 + 8 * U24 * (a + c1 + np.abs(xh) * c2))
+    _within("dx", dx, rdx, e + _unit(dt) * (np.abs(rdx) + e))
+    if dg is not None:
+        n = X.shape[0] + 4
+        _within("dgamma", dg, rdg, n * U24 * np.abs(D * xh).sum(axis=0) + (np.abs(D) * d_xh).sum(axis=0))
+    if db is not None:
+        _within("dbeta", db, rdb, (X.shape[0] + 4) * U24 * np.abs(D).sum(axis=0))
+
+
+@pytest.mark.parametrize("pad", [1, 8])
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_norm_rows_apart_in_place_and_without_parameters(dtype, pad):
+    torch = _torch()
+    M, N = 37, 520
+    x, _, _, dt = _norm_inputs(M, N, dtype, "float32", 14, pad=pad)
+    want, mean, rstd = _nan(M, N, dtype=dt), _nan(M), _nan(M)
+    C.compass_norm_forward(x.contiguous(), None, None, want, mean, rstd)
+    buf = _nan(M, N + pad, dtype=dt)
+    y = buf[:, :N]
+    y.copy_(x)
+    C.compass_norm_forward(y, None, None, y, mean, rstd)      # y is x
+    # the same numbers whichever threads hold a row: within the bounds of both
+    ry, rm, rr = E.norm_forward(_np(x), None, None, float(np.float32(1e-5)))
+    d_xh = _norm_tol(_np(x), None, rm, rr, ry)[2]
+    for got in (want, y):
+        _within("y", got, ry, d_xh + _unit(dt) * (np.abs(ry) + d_xh))
+    assert torch.isnan(buf[:, N:]).all()
+    dy = (_gen(15)(M, N + pad) * 0.01).to(dt)[:, :N]
+    D = dy.clone()
+    C.compass_norm_backward(dy, x, None, mean, rstd, dy, None, None, None)      # dx is dy, no sums wanted
+    _check_norm_backward(D, x, None, mean, rstd, dy, None, None, dt)
+
+
+def test_norm_constant_rows_and_rows_far_from_zero():
+    torch = _torch()
+    M, N = 6, 768
+    x = torch.full((M, N), 3.0, device="cuda")
+    x[3:] = 4096.0 + _gen(16)(3, N)
+    y, mean, rstd = _nan(M, N), _nan(M), _nan(M)
+    C.compass_norm_forward(x, None, None, y, mean, rstd)
+    assert torch.equal(y[:3], torch.zeros(3, N, device="cuda"))
+    ry, rm, rr = E.norm_forward(_np(x), None, None, float(np.float32(1e-5)))
+    d_mean, rel, d_xh = _norm_tol(_np(x), None, rm, rr, ry)
+    _within("mean", mean, rm, d_mean)
+    _within("y", y, ry, d_xh + 4 * U24 * np.abs(ry))
+
+
+def test_norm_gradient_against_differences():
+    torch = _torch()
+    M, N = 12, 200
+    x, g, b, dt = _norm_inputs(M, N, "float32", "float32", 17)
+    dy = _gen(18)(M, N)
+    y, mean, rstd = _nan(M, N), _nan(M), _nan(M)
+    C.compass_norm_forward(x, g, b, y, mean, rstd)
+    dx, dg, db = _nan(M, N), _nan(N), _nan(N)
+    C.compass_norm_backward(dy, x, g, mean, rstd, dx, dg, db, _scratch(C.compass_norm_workspace(M, N)))
+    X, G, B, D = _np(x), _np(g), _np(b), _np(dy)
+    f = lambda a, p, q: (E.norm_forward(a, p, q, float(np.float32(1e-5)))[0] * D).sum()  # noqa: E731
+    rng = np.random.default_rng(19)
+    for _ in range(4):
+        V, P, e = rng.standard_normal(X.shape), rng.standard_normal(N), 1e-5
+        for got, dif in (((_np(dx) * V).sum(), (f(X + e * V, G, B) - f(X - e * V, G, B)) / (2 * e)),
+                         ((_np(dg) * P).sum(), (f(X, G + e * P, B) - f(X, G - e * P, B)) / (2 * e)),
+                         ((_np(db) * P).sum(), (f(X, G, B + e * P) - f(X, G, B - e * P)) / (2 * e))):
+            # fp32 sums of 2400 products of order 1; the difference's own e^2 term
+            assert abs(got - dif) < 1e-3
+
+
+# ------------------------------------------------------------------- embedding
+def _ids(T, V, v0, seed, kind):
+    torch = _torch()
+    g = torch.Generator().manual_seed(seed)
+    if kind == "one":
+        ids = torch.full((T,), v0 + V // 2)
+    elif kind == "outside":
+        ids = torch.where(torch.arange(T) % 2 == 0, torch.tensor(-1), torch.tensor(v0 + V))
+    elif kind == "few":
+        ids = v0 + torch.randint(0, min(V, 3), (T,), generator=g)
+    else:
+        ids = torch.randint(-2, 2 * v0 + V + 2, (T,), generator=g)
+    return ids.long().cuda()
+
+
+EMBED = [(1, 1, 1, 0), (1, 7, 64, 0), (2, 5, 33, 5), (31, 9, 40, 0), (32, 3, 8, 0), (33, 2, 520, 2), (64, 70, 17, 0),
+         (65, 1000, 96, 1000), (500, 300, 1031, 300), (2049, 50, 264, 0), (4100, 70000, 24, 0), (20011, 130, 72, 10)]
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,V,K,v0", EMBED)
+def test_embed_forward(T, V, K, v0, dtype):
+    print(f"embed forward {T} {V} {K} {v0} {dtype}", flush=True)
+    torch = _torch()
+    dt = getattr(torch, dtype)
+    table = _gen(21)(V, K).to(dt)
+    ids = _ids(T, V, v0, 22, "any")
+    for scale in (4.0, float(np.float32(K ** 0.5))):
+        y = _nan(T, K, dtype=dt)
+        C.compass_embed_forward(ids, table, y, scale=scale, v0=v0)
+        ref = E.embed_forward(ids.cpu().numpy(), _np(table), scale, v0)
+        if scale == 4.0:   # exact
+            assert np.array_equal(_np(y), ref)
+        else:              # the fp32 product, then the element's type
+            _within("y", y, ref, np.abs(ref) * (_unit(dt) + 2 * U24))
+
+
+@pytest.mark.parametrize("kind", ["any", "one", "few", "outside"])
+@pytest.mark.parametrize("T,V,K,v0", EMBED)
+def test_embed_backward_integer_exact(T, V, K, v0, kind):
+    """Integers whose fp32 sums are exact: the rows' sums, bit for bit."""
+    print(f"embed backward {T} {V} {K} {v0} {kind}", flush=True)
+    torch = _torch()
+    g = torch.Generator(device="cuda").manual_seed(23)
+    ids = _ids(T, V, v0, 24, kind)
+    for dtype, gtype in (("bfloat16", "float32"), ("float32", "float32"), ("float32", "bfloat16"), ("bfloat16", "bfloat16")):
+        dy = torch.randint(-4, 5, (T, K), generator=g, device="cuda").to(getattr(torch, dtype))
+        d = _nan(V, K, dtype=getattr(torch, gtype))
+        C.compass_embed_backward(ids, dy, d, _scratch(C.compass_embed_workspace(T, V, K)), scale=0.5, v0=v0)
+        ref = E.embed_backward(ids.cpu().numpy(), _np(dy), V, 0.5, v0)
+        want = torch.from_numpy(ref).to(getattr(torch, gtype)).double().numpy()
+        assert np.array_equal(_np(d), want), (dtype, gtype, int((_np(d) != want).sum()))
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T,V,K,v0", [(500, 300, 1031, 300), (2049, 50, 264, 0), (20011, 130, 72, 10)])
+def test_embed_backward_seeded_and_accumulated(T, V, K, v0, dtype):
+    torch = _torch()
+    dt = getattr(torch, dtype)
+    ids = _ids(T, V, v0, 25, "any")
+    dy = _gen(26)(T, K + 3).to(dt)[:, :K]      # rows apart, unaligned
+    scale = 1.7
+    s32 = float(np.float32(scale))
+    ref = E.embed_backward(ids.cpu().numpy(), _np(dy), V, s32, v0)
+    mag = E.embed_backward(ids.cpu().numpy(), np.abs(_np(dy)), V, s32, v0)
+    count = E.embed_backward(ids.cpu().numpy(), np.ones((T, 1)), V, 1.0, v0)
+    ws = _scratch(C.compass_embed_workspace(T, V, K))
+    d = _nan(V, K, dtype=dt)
+    C.compass_embed_backward(ids, dy, d, ws, scale=scale, v0=v0)
+    e = (count + 2) * U24 * mag
+    _within("dtable", d, ref, e + _unit(dt) * (np.abs(ref) + e))
+    again = _nan(V, K, dtype=dt)
+    C.compass_embed_backward(ids, dy, again, ws, scale=scale, v0=v0)
+    assert torch.equal(d, again)
+    base = _gen(27)(V, K).to(dt)
+    base[(torch.from_numpy(count[:, 0]) == 0).cuda()] = float("nan")      # rows without tokens stay as they are
+    acc = base.clone()
+    C.compass_embed_backward(ids, dy, acc, ws, scale=scale, v0=v0, accumulate=True)
+    hit = count[:, 0] > 0
+    assert torch.isnan(acc[torch.from_numpy(~hit).cuda()]).all()
+    want = ref[hit] + _np(base)[hit]
+    e = e[hit] + 2 * U24 * np.abs(want)
+    _within("sum", acc[torch.from_numpy(hit).cuda()], want, e + _unit(dt) * (np.abs(want) + e))
+
+
+# ---------------------------------------------------------- streams and graphs
+def test_all_operators_on_a_side_stream_and_in_a_replayed_graph():
+    torch = _torch()
+    M, V, K = 200, 777, 264
+    H, W, t = _xent_inputs(M, V, K, 31)
+    x, g, b, dt = _norm_inputs(M, K, "bfloat16", "float32", 32)
+    bf = torch.bfloat16
+
+    def outputs():
+        return dict(lse=_nan(M), tl=_nan(M), loss=_nan(M), dH=_nan(M, K, dtype=bf), dW=_nan(V, K, dtype=bf),
+                    y=_nan(M, K, dtype=bf), mean=_nan(M), rstd=_nan(M), dx=_nan(M, K, dtype=bf), dg=_nan(K), db=_nan(K),
+                    e=_nan(M, K, dtype=bf), dt=_nan(V, K, dtype=bf))
+
+    grad = torch.full((M,), 1.0 / M, device="cuda")
+    ws = [_scratch(n) for n in (C.compass_xent_workspace(M, V, K), C.compass_xent_workspace(M, V, K, backward=True),
+                                C.compass_norm_workspace(M, K), C.compass_embed_workspace(M, V, K))]
+
+    def step(o, stream=None):
+        C.compass_embed_forward(t, W, o["e"], scale=2.0, stream=stream)
+        C.compass_norm_forward(x, g, b, o["y"], o["mean"], o["rstd"], stream=stream)
+        C.compass_xent_forward(H, W, t, o["lse"], o["tl"], o["loss"], ws[0], stream=stream)
+        C.compass_xent_backward(H, W, t, o["lse"], grad, o["dH"], o["dW"], ws[1], stream=stream)
+        C.compass_norm_backward(o["dH"], x, g, o["mean"], o["rstd"], o["dx"], o["dg"], o["db"], ws[2], stream=stream)
+        C.compass_embed_backward(t, o["dx"], o["dt"], ws[3], stream=stream)
+
+    want = outputs()
+    step(want)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = outputs()
+    torch.cuda.synchronize()
+    step(got, stream=side)
+    side.synchronize()
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    got = outputs()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(got)
+    for replay in range(4):
+        for k in got:
+            got[k].fill_(float("nan"))
+        x.mul_(1.0)   # eager work between the replays
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in want:
+            assert torch.equal(got[k], want[k]), (replay, k)
