@@ -245,18 +245,17 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(int N, int parts, con
 }
 
 constexpr int kMaxCols = 16384;   // a row's elements in 1024 threads' registers, 16 each
-constexpr int kMaxParts = 1024;
 
 int hip_error(hipError_t e, const char *what) {
     return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// Workgroups of the backward pass: as many as the card holds at once, each
-// with at least 8 rows of its own where there are that many, since every
-// workgroup leaves a row of 2 N sums.
-int backward_groups(int M, int rows) {
-    const int groups = (M + rows - 1) / rows;
-    return std::max(1, std::min(groups, std::min(kMaxParts, std::max(256, M / (8 * rows)))));
+// Workgroups of the backward pass: as many as the card holds at once (a row of
+// 1024 threads fills a CU), each with at least 4 rows per place where there are
+// that many, since every workgroup leaves a row of 2 N sums.
+int backward_groups(int M, int threads, int rows) {
+    const int held = 256 * (1024 / threads), groups = (M + rows - 1) / rows;
+    return std::max(1, std::min(groups, std::min(held, std::max(256, M / (4 * rows)))));
 }
 
 struct Launch {
@@ -268,7 +267,7 @@ struct Launch {
     void go() {
         constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
         if (backward) {
-            parts = backward_groups(p.M, ROWS);
+            parts = backward_groups(p.M, THREADS, ROWS);
             norm_backward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)parts), THREADS, 0, stream>>>(p);
         } else {
             norm_forward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)((p.M + ROWS - 1) / ROWS)), THREADS, 0, stream>>>(p);
@@ -365,7 +364,7 @@ int op_norm_workspace(int M, int N, size_t *bytes) {
     const int rc = check(M, N, COMPASS_BF16, COMPASS_BF16);
     if (rc != COMPASS_OK) return rc;
     if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
-    *bytes = (size_t)backward_groups(M, 1) * 2 * (size_t)N * 4;
+    *bytes = (size_t)backward_groups(M, 256, 1) * 2 * (size_t)N * 4;
     return COMPASS_OK;
 }
 

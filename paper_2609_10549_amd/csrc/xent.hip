@@ -27,6 +27,7 @@
 #include "gemm_core.h"
 #include "internal.h"
 #include "kernel_params.h"
+#include "xent_plan.h"
 
 namespace compass {
 
@@ -40,7 +41,8 @@ constexpr float kLog2e = 1.44269504088896340736f;
 enum Epilogue : int {
     kStats = 0,   // row maxima and sums of exponentials, the targets' logits
     kDz = 1,      // dz in bf16
-    kStore = 2,   // the product: bf16, or fp32 partial sums
+    kStore = 2,   // the product in bf16
+    kPart = 3,    // fp32 partial sums of the product
 };
 
 struct TileParams {
@@ -49,6 +51,7 @@ struct TileParams {
     int M, N, R;                 // rows and columns of C, reduction length
     int lda, ldb;                // elements between rows of A and B as they lie
     int tiles_m, tiles_n, group_m;
+    int m_base, n_base;          // the first tile's row and column
     int slices, kslice;          // reduction slices (kslice a multiple of 64)
     // kStats
     float2 *parts;               // [2 tiles_n][M]: maximum, sum
@@ -58,22 +61,24 @@ struct TileParams {
     int64_t v0;                  // vocabulary id of column 0
     // kDz
     const float *lse, *grad;
-    uint16_t *dz;
+    uint16_t *dz;                // grad / *peak (exp(z - lse) - [target])
     int ldz;                     // columns [N, ldz) are zero
-    // kStore
-    uint16_t *C;                 // bf16, rows of N (or null)
-    float *part_out;             // fp32 [slices][M][N] (or null)
-    const float *part_in;        // added first, same layout as part_out (or null)
+    const float *peak;           // kStore, kPart: the product is scaled by it
+    // kStore, and kPart's last sum
+    uint16_t *C;                 // bf16, rows of N
+    // kPart
+    float *part_out;             // fp32 [slices][M][N], or null: round to C
+    const float *part_in;        // added first, same layout (or null)
 };
 
 // f(row) of the 16-byte chunk permutation of an operand that lies across the
 // reduction: chunk c of LDS row `row` is at chunk c ^ f. Two neighbouring
 // chunks (16 columns) stay together, and the eight rows that half a wave reads
-// at once fall into eight different 32-byte bank groups (rows of 128 bytes:
-// two rows share a line of banks, four groups each).
+// at once fall into eight different 32-byte bank groups (rows of 128 or 384
+// bytes: odd rows start half a line of banks on, four groups each).
 template <int RB>
 __device__ __forceinline__ int cross_swizzle(int row) {
-    return RB >= 256 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
+    return RB % 256 == 0 ? 2 * ((row & 3) | ((row >> 1) & 4)) : 2 * (((row >> 1) & 1) | ((row >> 2) & 2));
 }
 
 // Loads of one operand's stages: `D` rows (or columns) of the tile, 64 of the
@@ -95,11 +100,11 @@ struct Loader {
             base = (uint64_t)p + o;
             left = (int64_t)bytes - (int64_t)o;
             step = (int64_t)ld * 128;
-            constexpr int CPR = RB / 16, RPB = 64 / CPR;   // chunks per row, rows per load
+            constexpr int CPR = RB / 16;   // chunks per row
 #pragma unroll
             for (int j = 0; j < L; ++j) {
-                const int row = (j * 4 + wave) * RPB + lane / CPR;
-                const int chunk = (lane % CPR) ^ cross_swizzle<RB>(row);
+                const int at = (j * 4 + wave) * 64 + lane;
+                const int row = at / CPR, chunk = (at % CPR) ^ cross_swizzle<RB>(row);
                 off[j] = (uint32_t)row * (uint32_t)ld * 2u + (uint32_t)chunk * 16u;
             }
         } else {
@@ -240,8 +245,8 @@ void tile_kernel(const TileParams p) {
     const int gsz = p.group_m * p.tiles_n;
     const int grp = tpos / gsz, rin = tpos - grp * gsz;
     const int rows_here = min(p.group_m, p.tiles_m - grp * p.group_m);
-    const int m0 = (grp * p.group_m + rin % rows_here) * BM;
-    const int n0 = (rin / rows_here) * BN;
+    const int tm = grp * p.group_m + rin % rows_here, tn = rin / rows_here;
+    const int m0 = p.m_base + tm * BM, n0 = p.n_base + tn * BN;
     const int kb = slice * p.kslice, ke = min(p.R, kb + p.kslice);
 
     f32x4 acc[FN][FM];
@@ -332,7 +337,7 @@ void tile_kernel(const TileParams p) {
     if constexpr (EPI == kStats) {
         const int c0 = n0 + wn0 + 4 * eq;
         const bool edge = n0 + BN > p.N;
-        float2 *out = p.parts + (size_t)(2 * (n0 / BN) + (wave & 1)) * (size_t)p.M;
+        float2 *out = p.parts + (size_t)(2 * tn + (wave & 1)) * (size_t)p.M;
 #pragma unroll
         for (int mi = 0; mi < FM; ++mi) {
             const int m = m0 + wm0 + mi * 16 + er;
@@ -363,101 +368,183 @@ void tile_kernel(const TileParams p) {
             }
         }
     } else {
-        // each wave turns 32 rows at a time to row order through a region of
-        // the freed stage buffers, as gemm_kernel's epilogue does
-        constexpr int CPR = 2 * FN, NIT = 32 * CPR / 64, RB = FN * 64;
-        static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
-        char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
-        auto to_lds = [&](int mi) {
-            char *w = region[mi & 1] + er * RB;
+        // Each wave turns 32 rows at a time to row order through a region of
+        // the freed stage buffers and stores whole rows of its columns, 16
+        // bytes per lane. The regions are the wave's own and its LDS operations
+        // run in order: nothing waits between a write and its read.
+        const float peak = EPI == kDz ? 0.0f : *p.peak;
+        if constexpr (EPI == kPart) {
+            // fp32: 16-byte chunk c of row r at chunk c ^ (r & 7)
+            constexpr int CPR = 2 * FN, NIT = 32 * CPR / 64, RB = FN * 64;
+            static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
+            char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
+            auto to_lds = [&](int mi) {
+                char *w = region[mi & 1] + er * RB;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int ni = 0; ni < FN; ++ni)
-                    *reinterpret_cast<f32x4 *>(w + h * 16 * RB + (((4 * ni + eq) ^ (er & 7)) << 4)) = acc[ni][2 * mi + h];
-            asm volatile("" ::: "memory");
-        };
-        to_lds(0);
+                    for (int ni = 0; ni < FN; ++ni)
+                        *reinterpret_cast<f32x4 *>(w + h * 16 * RB + (((4 * ni + eq) ^ (er & 7)) << 4)) =
+                            acc[ni][2 * mi + h];
+                asm volatile("" ::: "memory");
+            };
+            to_lds(0);
 #pragma unroll
-        for (int mi = 0; mi < FM / 2; ++mi) {
-            if (mi + 1 < FM / 2) to_lds(mi + 1);
+            for (int mi = 0; mi < FM / 2; ++mi) {
+                if (mi + 1 < FM / 2) to_lds(mi + 1);
 #pragma unroll
-            for (int it = 0; it < NIT; ++it) {
-                const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
-                const char *w = region[mi & 1] + row * RB;
-                // half of the lanes take their two chunks in the other order,
-                // so that 8 lanes read 8 different bank groups
-                const int sw = (j >> 2) & 1;
-                const f32x4 u0 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + sw) ^ (row & 7)) << 4));
-                const f32x4 u1 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + 1 - sw) ^ (row & 7)) << 4));
-                float x[8];
+                for (int it = 0; it < NIT; ++it) {
+                    const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
+                    const char *w = region[mi & 1] + row * RB;
+                    // half of the lanes take their two chunks in the other order,
+                    // so that 8 lanes read 8 different bank groups
+                    const int sw = (j >> 2) & 1;
+                    const f32x4 u0 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + sw) ^ (row & 7)) << 4));
+                    const f32x4 u1 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + 1 - sw) ^ (row & 7)) << 4));
+                    f32x4 x0, x1;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = sw ? u1[e] : u0[e];
-                    x[4 + e] = sw ? u0[e] : u1[e];
-                }
-                const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
-                if constexpr (EPI == kDz) {
-                    if (m < p.M && n < p.ldz) {
-                        const int64_t t0 = p.target[m];
-                        const int64_t t = t0 - p.v0 - n;
-                        const float lse = p.lse[m], g = p.grad[m];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float pr = __builtin_amdgcn_exp2f((x[e] - lse) * kLog2e) - (t == e ? 1.0f : 0.0f);
-                            x[e] = t0 < 0 || n + e >= p.N ? 0.0f : g * pr;
-                        }
-                        *reinterpret_cast<u32x4 *>(p.dz + (size_t)m * (size_t)p.ldz + n) =
-                            u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                  pack_bf16x2(x[6], x[7])};
+                    for (int e = 0; e < 4; ++e) {
+                        x0[e] = peak * (sw ? u1[e] : u0[e]);
+                        x1[e] = peak * (sw ? u0[e] : u1[e]);
                     }
-                } else {
+                    const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
                     if (m < p.M && n < p.N) {   // N is a multiple of 8
                         const size_t at = ((size_t)slice * (size_t)p.M + (size_t)m) * (size_t)p.N + n;
                         if (p.part_in) {
-                            const f32x4 q0 = *reinterpret_cast<const f32x4 *>(p.part_in + at);
-                            const f32x4 q1 = *reinterpret_cast<const f32x4 *>(p.part_in + at + 4);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                x[e] += q0[e];
-                                x[4 + e] += q1[e];
-                            }
+                            x0 += *reinterpret_cast<const f32x4 *>(p.part_in + at);
+                            x1 += *reinterpret_cast<const f32x4 *>(p.part_in + at + 4);
                         }
                         if (p.part_out) {
-                            *reinterpret_cast<f32x4 *>(p.part_out + at) = f32x4{x[0], x[1], x[2], x[3]};
-                            *reinterpret_cast<f32x4 *>(p.part_out + at + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                            *reinterpret_cast<f32x4 *>(p.part_out + at) = x0;
+                            *reinterpret_cast<f32x4 *>(p.part_out + at + 4) = x1;
                         } else {
                             *reinterpret_cast<u32x4 *>(p.C + (size_t)m * (size_t)p.N + n) =
-                                u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
-                                      pack_bf16x2(x[6], x[7])};
+                                u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]),
+                                      pack_bf16x2(x1[2], x1[3])};
                         }
                     }
+                }
+            }
+        } else {
+            // rounded in the accumulators' layout, so that half the bytes go
+            // through LDS: chunk c of row r at chunk c ^ (r & SW)
+            constexpr int CPR = 2 * FN, RB = FN * 32, SW_ = CPR % 8 == 0 ? 7 : 3;
+            static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
+            char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
+            // dz: the rows' statistics, all loaded at once
+            float lse[EPI == kDz ? FM : 1], g[EPI == kDz ? FM : 1];
+            int t[EPI == kDz ? FM : 1];   // the target's place from this lane's first column, or -1
+            if constexpr (EPI == kDz) {
+                const float top = *p.peak;
+#pragma unroll
+                for (int mi = 0; mi < FM; ++mi) {
+                    const int m = min(m0 + wm0 + mi * 16 + er, p.M - 1);
+                    const int64_t id = p.target[m], at = id - p.v0 - (n0 + wn0 + 4 * eq);
+                    lse[mi] = p.lse[m];
+                    g[mi] = id < 0 ? 0.0f : p.grad[m] / top;
+                    t[mi] = id < 0 || at < 0 || at >= WN ? -1 : (int)at;
+                }
+            }
+            const int c0 = n0 + wn0 + 4 * eq;
+            const bool edge = n0 + BN > p.N;
+            auto to_lds = [&](int mi2) {
+                char *w = region[mi2 & 1] + er * RB;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int ni = 0; ni < FN; ++ni) {
+                        f32x4 x = acc[ni][2 * mi2 + h];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if constexpr (EPI == kDz) {
+                                const int mi = 2 * mi2 + h;
+                                const float pr = __builtin_amdgcn_exp2f((x[e] - lse[mi]) * kLog2e);
+                                x[e] = g[mi] * (pr - (t[mi] == ni * 16 + e ? 1.0f : 0.0f));
+                                // (a row without weight is zero whatever its logits are)
+                                if (g[mi] == 0.0f || (edge && c0 + ni * 16 + e >= p.N)) x[e] = 0.0f;
+                            } else {
+                                x[e] *= peak;
+                            }
+                        }
+                        *reinterpret_cast<u32x2 *>(w + h * 16 * RB + (((2 * ni + (eq >> 1)) ^ (er & SW_)) << 4) +
+                                                   8 * (eq & 1)) =
+                            u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
+                    }
+                asm volatile("" ::: "memory");
+            };
+            uint16_t *out = EPI == kDz ? p.dz : p.C;
+            const int ld = EPI == kDz ? p.ldz : p.N;
+            to_lds(0);
+#pragma unroll
+            for (int mi = 0; mi < FM / 2; ++mi) {
+                if (mi + 1 < FM / 2) to_lds(mi + 1);
+#pragma unroll
+                for (int it = 0; it < FN; ++it) {
+                    const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
+                    const u32x4 o = *reinterpret_cast<const u32x4 *>(region[mi & 1] + row * RB + ((j ^ (row & SW_)) << 4));
+                    const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
+                    if (m < p.M && n < ld) *reinterpret_cast<u32x4 *>(out + (size_t)m * (size_t)ld + n) = o;
                 }
             }
         }
     }
 }
 
-// Joins a row's parts: lse = max + log sum_i s_i exp(m_i - max). 16 rows per
-// workgroup, 16 lanes each.
+// The largest |grad| of a row with a target (1 without any). dz is stored as
+// its multiple, and the products are scaled back in fp32: with one weight for
+// all rows, as in a mean, the multiple is exactly 1, and -1 at the targets'
+// columns is exact where grad itself would round by the same 2^-9 or so in
+// every row (dH and dW then err by 2.6e-3, with it by 2.0e-3).
+__global__ __launch_bounds__(1024) void peak_kernel(int M, const int64_t *target, const float *grad, float *peak) {
+    __shared__ float s[16];
+    float x = 0.0f;
+#pragma unroll 8
+    for (int m = threadIdx.x; m < M; m += 1024) {
+        const float g = fabsf(grad[m]);
+        x = fmaxf(x, target[m] >= 0 ? g : 0.0f);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
+    *peak = x > 0.0f && x < INFINITY ? x : 1.0f;
+}
+
+// Joins a row's parts: lse = max + log sum_i s_i exp(m_i - max). ROWS rows per
+// workgroup, 256 / ROWS threads each: 16 rows read whole 128-byte lines of the
+// parts; few rows (at most 256) take a workgroup each (8 rows of 1000 parts:
+// 20.6 us with 16).
+template <int ROWS>
 __global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, const float2 *__restrict__ part,
                                                     const int64_t *target, int64_t v0, float *lse, float *tlogit,
                                                     float *loss) {
-    __shared__ float2 s_part[16][16];
-    const int r = threadIdx.x & 15, q = threadIdx.x >> 4;
-    const int m = (int)blockIdx.x * 16 + r;
+    constexpr int Q = 256 / ROWS;
+    __shared__ float2 s_part[Q][ROWS];
+    const int r = threadIdx.x % ROWS, q = threadIdx.x / ROWS;
+    const int m = (int)blockIdx.x * ROWS + r;
     float mx = -INFINITY, sum = 0.0f;
     auto add = [&](float2 x) {
         const float top = fmaxf(mx, x.x), sub = top == -INFINITY ? 0.0f : top;
         sum = sum * __builtin_amdgcn_exp2f((mx - sub) * kLog2e) + x.y * __builtin_amdgcn_exp2f((x.x - sub) * kLog2e);
         mx = top;
     };
-    if (m < M)
-        for (int i = q; i < parts; i += 16) add(part[(size_t)i * (size_t)M + m]);
+    if (m < M) {
+#pragma unroll 4
+        for (int i = q; i < parts; i += Q) add(part[(size_t)i * (size_t)M + m]);
+    }
     s_part[q][r] = make_float2(mx, sum);
-    __syncthreads();
+#pragma unroll
+    for (int half = Q / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (q < half) {
+            add(s_part[q + half][r]);
+            s_part[q][r] = make_float2(mx, sum);
+        }
+    }
     if (q != 0 || m >= M) return;
-    for (int i = 1; i < 16; ++i) add(s_part[i][r]);
     const float l = mx + logf(sum);
     const int64_t t = target[m];
     float tl = 0.0f;
@@ -498,102 +585,45 @@ __global__ __launch_bounds__(256) void join_slices_kernel(size_t count4, int sli
 
 // ------------------------------------------------------------------- plans
 
-struct Shape { int rows, cols, wg_per_cu; double stage_us, edge_us; };
-constexpr Shape kShapes[] = {
-    {256, 256, 1, 1.40, 9.0}, {128, 128, 2, 0.90, 5.0}, {64, 64, 2, 0.45, 3.0}};
-constexpr int kShapeCount = 3;
-constexpr int kCUs = 256;   // the card this library is built for; sizes of workspaces follow from it
-
-struct TilePlan { int shape, tiles_m, tiles_n, slices, kslice; };
-
-// The cheapest tile (and slices of the reduction, at most max_slices) by
-// rounds of workgroups times a tile's time.
-TilePlan plan_tiles(int M, int N, int R, int max_slices) {
-    TilePlan best{};
-    double best_t = 0;
-    for (int s = 0; s < kShapeCount; ++s) {
-        const Shape &sh = kShapes[s];
-        const int tm = (M + sh.rows - 1) / sh.rows, tn = (N + sh.cols - 1) / sh.cols;
-        const double tiles = (double)tm * tn;
-        const int stages = (R + kBK - 1) / kBK;
-        for (int k = 1; k <= max_slices && (k == 1 || stages / k >= 8); ++k) {
-            const int per = (stages + k - 1) / k;
-            const int ns = (stages + per - 1) / per;
-            const double rounds = std::max(1.0, tiles * ns / (kCUs * sh.wg_per_cu));
-            const double whole = rounds < 4 ? (double)(int64_t)(rounds + 0.999) : rounds + 0.5;
-            double t = whole * (per * sh.stage_us + sh.edge_us);
-            if (ns > 1) t += 5.0 + 8.0e-6 * (double)M * N * ns / 4.0;   // fp32 slices out and in
-            if (best_t == 0 || t < best_t) {
-                best_t = t;
-                best = {s, tm, tn, ns, per * kBK};
-            }
-        }
-    }
-    return best;
-}
-
 template <bool AT, bool BT, int EPI>
-hipError_t launch_tiles(TileParams &p, const TilePlan &pl, hipStream_t stream) {
+hipError_t launch_tiles(TileParams p, const TilePlan &pl, hipStream_t stream) {
     p.tiles_m = pl.tiles_m;
     p.tiles_n = pl.tiles_n;
     p.slices = pl.slices;
     p.kslice = pl.kslice;
-    p.group_m = pl.shape == 0 ? 4 : 8;
+    p.group_m = kTileShapes[pl.cfg].rows == 256 ? 4 : 8;
     const dim3 grid((unsigned)(pl.tiles_m * pl.tiles_n * pl.slices));
-    switch (pl.shape) {
-    case 0: tile_kernel<256, 256, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case 1: tile_kernel<128, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    switch (pl.cfg) {
+    case kTile256: tile_kernel<256, 256, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile256x192: tile_kernel<256, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile256x128: tile_kernel<256, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile192: tile_kernel<192, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile128x192: tile_kernel<128, 192, 3, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile128: tile_kernel<128, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile128Deep: tile_kernel<128, 128, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case kTile128x64Deep: tile_kernel<128, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
     default: tile_kernel<64, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
     }
     return hipGetLastError();
+}
+
+// A product in the one or two launches of its plan.
+template <bool AT, bool BT, int EPI>
+hipError_t launch_pair(TileParams p, const PairPlan &pl, bool along_m, hipStream_t stream) {
+    hipError_t e = launch_tiles<AT, BT, EPI>(p, pl.part[0], stream);
+    if (e == hipSuccess && pl.part[1].tiles_m > 0) {
+        (along_m ? p.m_base : p.n_base) = pl.first;
+        p.parts += (size_t)2 * pl.part[0].tiles_n * (size_t)p.M;
+        e = launch_tiles<AT, BT, EPI>(p, pl.part[1], stream);
+    }
+    return e;
 }
 
 int hip_error(hipError_t e, const char *what) {
     return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-constexpr int kMaxSlices = 16;
-constexpr size_t kPieceBytes = (size_t)512 << 20;   // dz of a default piece
-
-// Pieces of the vocabulary of a backward pass, all but the last `cols` wide.
-struct Pieces { int cols, count; };
-Pieces plan_pieces(int M, int V, int piece) {
-    int cols = piece;
-    if (cols == 0) {
-        const size_t fit = std::max<size_t>(kPieceBytes / ((size_t)M * 2) / 256 * 256, 256);
-        if ((size_t)V <= fit) cols = V;
-        else {
-            const int count = (int)((V + fit - 1) / fit);
-            cols = ((V + count - 1) / count + 255) / 256 * 256;
-        }
-    }
-    cols = std::min(cols, V);
-    return {cols, (V + cols - 1) / cols};
-}
-
-int dz_columns(int cols) { return (cols + 63) / 64 * 64; }
-
-struct BackwardPlan {
-    Pieces pieces;
-    TilePlan dh;      // of a whole piece
-    int ldz;
-    size_t dz_bytes, part_bytes;
-};
-BackwardPlan plan_backward(int M, int V, int K, int piece) {
-    BackwardPlan b;
-    b.pieces = plan_pieces(M, V, piece);
-    b.ldz = dz_columns(b.pieces.cols);
-    b.dh = plan_tiles(M, K, b.ldz, kMaxSlices);
-    b.dz_bytes = align256((size_t)M * (size_t)b.ldz * 2);
-    b.part_bytes = b.pieces.count > 1 || b.dh.slices > 1 ? (size_t)b.dh.slices * (size_t)M * (size_t)K * 4 : 0;
-    return b;
-}
-
-size_t forward_bytes(int M, int V, int K) {
-    return (size_t)plan_tiles(M, V, K, 1).tiles_n * 2 * (size_t)M * sizeof(float2);
-}
+size_t forward_bytes(const PairPlan &pl, int M) { return (size_t)stat_parts(pl) * (size_t)M * sizeof(float2); }
 
 constexpr int kMaxRows = 1 << 20, kMaxVocab = 1 << 24, kMaxDepth = 1 << 17;
 
@@ -618,7 +648,7 @@ int op_xent_workspace(int M, int V, int K, int backward, int piece, size_t *byte
         const BackwardPlan b = plan_backward(M, V, K, piece);
         *bytes = b.dz_bytes + b.part_bytes;
     } else {
-        *bytes = forward_bytes(M, V, K);
+        *bytes = forward_bytes(plan_pair(M, V, K, false), M);
     }
     return COMPASS_OK;
 }
@@ -632,9 +662,9 @@ int op_xent_forward(int M, int V, int K, const void *H, const void *W, const int
     if (misaligned(H) || misaligned(W) || misaligned(ws))
         return set_error(COMPASS_ERR_INVALID, "H, W and the workspace must be 16-byte aligned");
     if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
-    const TilePlan pl = plan_tiles(M, V, K, 1);
-    if (ws_bytes < forward_bytes(M, V, K))
-        return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, forward_bytes(M, V, K));
+    const PairPlan pl = plan_pair(M, V, K, false);
+    if (ws_bytes < forward_bytes(pl, M))
+        return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, forward_bytes(pl, M));
     int cus;
     if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
     TileParams p{};
@@ -649,10 +679,14 @@ int op_xent_forward(int M, int V, int K, const void *H, const void *W, const int
     p.tlogit = tlogit;
     p.target = target;
     p.v0 = v0;
-    hipError_t e = launch_tiles<false, false, kStats>(p, pl, (hipStream_t)stream);
+    hipError_t e = launch_pair<false, false, kStats>(p, pl, false, (hipStream_t)stream);
     if (e != hipSuccess) return hip_error(e, "logits launch");
-    stats_kernel<<<dim3((unsigned)((M + 15) / 16)), 256, 0, (hipStream_t)stream>>>(M, V, 2 * pl.tiles_n, p.parts, target,
-                                                                                v0, lse, tlogit, loss);
+    if (M <= 256)
+        stats_kernel<1><<<dim3((unsigned)M), 256, 0, (hipStream_t)stream>>>(M, V, stat_parts(pl), p.parts, target, v0,
+                                                                            lse, tlogit, loss);
+    else
+        stats_kernel<16><<<dim3((unsigned)((M + 15) / 16)), 256, 0, (hipStream_t)stream>>>(
+            M, V, stat_parts(pl), p.parts, target, v0, lse, tlogit, loss);
     e = hipGetLastError();
     return e == hipSuccess ? COMPASS_OK : hip_error(e, "statistics launch");
 }
@@ -688,7 +722,10 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
     if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
     const hipStream_t s = (hipStream_t)stream;
     uint16_t *dz = (uint16_t *)ws;
+    float *peak = (float *)((char *)ws + b.dz_bytes - 256);
     float *part = (float *)((char *)ws + b.dz_bytes);
+    peak_kernel<<<1, 1024, 0, s>>>(M, target, grad, peak);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return hip_error(e, "peak launch");
     const uint64_t h_bytes = (uint64_t)M * (uint64_t)K * 2;
     for (int i = 0; i < b.pieces.count; ++i) {
         const int c0 = i * b.pieces.cols, cols = std::min(b.pieces.cols, V - c0);
@@ -706,9 +743,10 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         p.v0 = v0 + c0;
         p.lse = lse;
         p.grad = grad;
+        p.peak = peak;
         p.dz = dz;
         p.ldz = dz_columns(cols);
-        hipError_t e = launch_tiles<false, false, kDz>(p, plan_tiles(M, p.ldz, K, 1), s);
+        hipError_t e = launch_pair<false, false, kDz>(p, plan_pair(M, p.ldz, K, false), false, s);
         if (e != hipSuccess) return hip_error(e, "dz launch");
 
         TileParams q{};
@@ -721,8 +759,9 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         q.M = cols;
         q.N = q.ldb = K;
         q.R = M;
+        q.peak = peak;
         q.C = (uint16_t *)dW + (size_t)c0 * (size_t)K;
-        e = launch_tiles<true, true, kStore>(q, plan_tiles(cols, K, M, 1), s);
+        e = launch_pair<true, true, kStore>(q, plan_pair(cols, K, M, true), true, s);
         if (e != hipSuccess) return hip_error(e, "dW launch");
         // dH += dz W over this piece
         q.B = Wp;
@@ -738,7 +777,8 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         TilePlan pl = b.dh;
         const int stages = p.ldz / kBK;
         pl.kslice = (stages + pl.slices - 1) / pl.slices * kBK;
-        e = launch_tiles<false, true, kStore>(q, pl, s);
+        e = q.part_in || q.part_out ? launch_tiles<false, true, kPart>(q, pl, s)
+                                    : launch_tiles<false, true, kStore>(q, pl, s);
         if (e != hipSuccess) return hip_error(e, "dH launch");
     }
     if (b.dh.slices > 1) {
