@@ -65,7 +65,7 @@ __device__ __forceinline__ void store_row(T *row, int i, int N, const float (&f)
         Pack<T, V> p;
 #pragma unroll
         for (int e = 0; e < V; ++e) p.e[e] = from_f32<T>(f[e]);
-        *reinterpret_cast<Pack<T, V> *>(row + i) = p;
+        store_stream<T, V>(row + i, p);
     }
 }
 

@@ -26,6 +26,36 @@ __device__ __forceinline__ Bf16 from_f32<Bf16>(float x) {   // round to nearest 
     return Bf16{__builtin_bit_cast(uint16_t, (__bf16)x)};
 }
 
+// Loads and stores that pass through the caches without staying (whole vectors;
+// single elements go the ordinary way, lanes share their lines). An output of
+// more than the caches hold would otherwise be allocated line by line and
+// written back later: what a kernel measured with and without stands there.
+typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
+template <class T, int V>
+__device__ __forceinline__ void store_stream(T *p, const Pack<T, V> &o) {
+    constexpr int N = sizeof(T) * V / 16;
+    if constexpr (sizeof(T) * V % 16 == 0 && N > 0) {
+        struct Quads { u32x4_ q[N]; };
+        const Quads q = __builtin_bit_cast(Quads, o);
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_nontemporal_store(q.q[i], reinterpret_cast<u32x4_ *>(p) + i);
+    } else {
+        *reinterpret_cast<Pack<T, V> *>(p) = o;
+    }
+}
+template <class T, int V>
+__device__ __forceinline__ Pack<T, V> load_stream(const T *p) {
+    constexpr int N = sizeof(T) * V / 16;
+    if constexpr (sizeof(T) * V % 16 == 0 && N > 0) {
+        struct Quads { u32x4_ q[N]; } q;
+#pragma unroll
+        for (int i = 0; i < N; ++i) q.q[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_ *>(p) + i);
+        return __builtin_bit_cast(Pack<T, V>, q);
+    } else {
+        return *reinterpret_cast<const Pack<T, V> *>(p);
+    }
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xF, 0xF, true));
