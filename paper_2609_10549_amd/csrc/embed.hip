@@ -26,59 +26,43 @@ namespace {
 constexpr int kRun = 32;
 
 // How a kernel's workgroups of 256 threads cover rows of K elements: groups of
-// 2^shift threads, each thread ITEMS vectors of a row's columns; blockIdx.y
-// counts the column blocks of rows that one group does not cover.
+// 2^shift threads, a vector of V elements each; blockIdx.y counts the column
+// blocks of rows that one group does not cover.
 struct Cover {
     int shift;
     __device__ __forceinline__ int group(int wg) const { return (wg << (8 - shift)) + ((int)threadIdx.x >> shift); }
-    // first element of this thread's vector i of V elements
-    template <int V, int ITEMS>
-    __device__ __forceinline__ int column(int i) const {
-        const int lane = (int)threadIdx.x & ((1 << shift) - 1);
-        return ((((int)blockIdx.y * ITEMS + i) << shift) + lane) * V;
+    template <int V>
+    __device__ __forceinline__ int column() const {
+        return (((int)blockIdx.y << shift) + ((int)threadIdx.x & ((1 << shift) - 1))) * V;
     }
 };
 
-// (32768 tokens, 50257 x 4096 bf16, token frequencies as 1 / rank, ordinary ->
-// streaming stores: lookup 86 -> 60 us, gradient 183 -> 150)
-template <class T, int V>
-__device__ __forceinline__ void store_vec(T *p, const float (&f)[V]) {
-    Pack<T, V> o;
-#pragma unroll
-    for (int e = 0; e < V; ++e) o.e[e] = from_f32<T>(f[e]);
-    store_stream<T, V>(p, o);
-}
-
 // TOKENS tokens per group, their rows in flight together.
-template <class T, int V, int ITEMS, int TOKENS>
+//
+// Bound by memory. 32768 tokens, 50257 x 4096 bf16, token frequencies as
+// 1 / rank: 86 us with ordinary stores, 60 with streaming ones.
+template <class T, int V, bool LOOSE, int TOKENS>
 __global__ __launch_bounds__(256) void lookup_kernel(Cover cov, int tokens, int K, int64_t v0, int vocab,
                                                      const int64_t *__restrict__ ids, const T *__restrict__ table,
                                                      int64_t ldt, float scale, T *y, int64_t ldy) {
-    const int t0 = cov.group((int)blockIdx.x) * TOKENS;
-    if (t0 >= tokens) return;
-    Pack<T, V> p[TOKENS][ITEMS];
+    const int t0 = cov.group((int)blockIdx.x) * TOKENS, c = cov.column<V>();
+    if (t0 >= tokens || c >= K) return;
+    Pack<T, V> p[TOKENS];
     bool inside[TOKENS];
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
         const int64_t row = t0 + j < tokens ? ids[t0 + j] - v0 : -1;
         inside[j] = row >= 0 && row < vocab;
-#pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int c = cov.column<V, ITEMS>(i);
-            if (inside[j] && c < K) p[j][i] = *reinterpret_cast<const Pack<T, V> *>(table + row * ldt + c);
-        }
+        if (inside[j]) p[j] = load_pack<T, V, LOOSE>(table + row * ldt, c, K);
     }
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
         if (t0 + j >= tokens) return;
+        float f[V];
+        unpack(p[j], f);
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i) {
-            const int c = cov.column<V, ITEMS>(i);
-            float f[V];
-#pragma unroll
-            for (int e = 0; e < V; ++e) f[e] = inside[j] ? to_f32(p[j][i].e[e]) * scale : 0.0f;
-            if (c < K) store_vec<T, V>(y + (int64_t)(t0 + j) * ldy + c, f);
-        }
+        for (int e = 0; e < V; ++e) f[e] = inside[j] ? f[e] * scale : 0.0f;
+        store_pack<T, V, LOOSE>(y + (int64_t)(t0 + j) * ldy, c, K, f);
     }
 }
 
@@ -173,36 +157,31 @@ __global__ __launch_bounds__(256) void runs_kernel(int T, int vocab, const int *
     first[v] = lo;
 }
 
-// f += dy of the sorted positions [lo, hi), in order, kAhead rows in flight;
-// the lanes of a group (or of its wave) fetch the token indices together.
+// f += the vector at column c of dy of the sorted positions [lo, hi), in order,
+// kAhead rows in flight; the lanes of a group (or of its wave) fetch the token
+// indices together.
 constexpr int kAhead = 4;
-template <class T, int V, int ITEMS>
-__device__ __forceinline__ void add_rows(float (&f)[ITEMS][V], const Cover &cov, int K, const int *__restrict__ order,
+template <class T, int V, bool LOOSE>
+__device__ __forceinline__ void add_rows(float (&f)[V], int shift, int c, int K, const int *__restrict__ order,
                                          const T *__restrict__ dy, int64_t ld, int lo, int hi) {
-    const int width = 1 << min(cov.shift, 6), lane = (int)threadIdx.x & (width - 1);
+    const int width = 1 << min(shift, 6), lane = (int)threadIdx.x & (width - 1);
     for (int base = lo; base < hi; base += width) {
         const int mine = base + lane < hi ? order[base + lane] : 0;
         const int n = min(width, hi - base);
         for (int i = 0; i < n; i += kAhead) {
-            Pack<T, V> p[kAhead][ITEMS];
+            Pack<T, V> p[kAhead];
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int tok = __shfl(mine, i + j, width);   // (width is a multiple of kAhead)
-                if (i + j < n) {
-#pragma unroll
-                    for (int q = 0; q < ITEMS; ++q) {
-                        const int c = cov.column<V, ITEMS>(q);
-                        if (c < K) p[j][q] = *reinterpret_cast<const Pack<T, V> *>(dy + (int64_t)tok * ld + c);
-                    }
-                }
+                if (i + j < n) p[j] = load_pack<T, V, LOOSE>(dy + (int64_t)tok * ld, c, K);
             }
 #pragma unroll
             for (int j = 0; j < kAhead; ++j)
                 if (i + j < n) {
+                    float d[V];
+                    unpack(p[j], d);
 #pragma unroll
-                    for (int q = 0; q < ITEMS; ++q)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) f[q][e] += to_f32(p[j][q].e[e]);
+                    for (int e = 0; e < V; ++e) f[e] += d[e];
                 }
         }
     }
@@ -213,7 +192,8 @@ struct Gradient {
     int T, K, V;
     int blocks;                     // kRun sorted positions each
     const int *order, *sorted, *first;
-    float *part;                    // [blocks][K]
+    float *part;                    // [blocks][ldp]
+    int ldp;
     const void *dy;
     int64_t ld;
     float scale;
@@ -221,58 +201,50 @@ struct Gradient {
     int64_t ldt;
 };
 
-template <class G, int V, bool ACC>
-__device__ __forceinline__ void put_vec(const Gradient &g, int row, int c, float (&f)[V]) {
-    G *out = (G *)g.dtable + (int64_t)row * g.ldt + c;
+// A table row's sums from column c on, scaled, to the table or onto it.
+template <class G, int V, bool LOOSE, bool ACC>
+__device__ __forceinline__ void put_row(const Gradient &g, int row, int c, float (&f)[V]) {
+    G *out = (G *)g.dtable + (int64_t)row * g.ldt;
 #pragma unroll
     for (int e = 0; e < V; ++e) f[e] *= g.scale;
     if constexpr (ACC) {
-        const Pack<G, V> o = load_stream<G, V>(out);
+        float o[V];
+        unpack(load_pack<G, V, LOOSE, true>(out, c, g.K), o);
 #pragma unroll
-        for (int e = 0; e < V; ++e) f[e] += to_f32(o.e[e]);
+        for (int e = 0; e < V; ++e) f[e] += o[e];
     }
-    store_vec<G, V>(out, f);
-}
-
-template <class G, int V, bool ACC, int ITEMS>
-__device__ __forceinline__ void put_row(const Gradient &g, int row, float (&f)[ITEMS][V]) {
-#pragma unroll
-    for (int q = 0; q < ITEMS; ++q) {
-        const int c = g.cov.column<V, ITEMS>(q);
-        if (c < g.K) put_vec<G, V, ACC>(g, row, c, f[q]);
-    }
+    store_pack<G, V, LOOSE>(out, c, g.K, f);
 }
 
 // One launch of three kinds of groups, each kind rounded up to a workgroup:
 //   blocks: the sum of a block of kRun sorted positions that lies inside one run;
 //   tokens: kAhead sorted positions; writes the table rows of the runs that
 //     begin there, but for one that holds such a block;
-//   zeros (not with accumulate): kZeroRows table rows, those without tokens.
-// In that order: reads and writes dealt evenly over the launch took longer
-// (32768 distinct tokens, 50257 x 4096 bf16: 220 us for the whole gradient,
-// 200 in this order).
+//   zeros (not with ACC): kZeroRows table rows, those without tokens.
+// In that order: reads and writes dealt evenly over the launch took longer.
+//
+// Bound by memory. 32768 distinct tokens, 50257 x 4096 bf16 (680 MB), the whole
+// gradient: 220 us with the kinds dealt evenly, 200 in this order, 168 with 4
+// rows in flight per thread in place of 8 (more waves; two vectors per thread
+// in place of one: 229), 129 with streaming stores of the table. Adding to a
+// table that is there (ACC), the loads of dy and the table stream too: 187 ->
+// 166 us (without ACC that costs: 129 -> 150).
 constexpr int kZeroRows = 8;
-template <class T, class G, int V, bool ACC, int ITEMS>
+template <class T, class G, int V, bool LOOSE, bool ACC>
 __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
     const int per = 256 >> g.cov.shift;
     const int block_wgs = (g.blocks + per - 1) / per, token_wgs = ((g.T + kAhead - 1) / kAhead + per - 1) / per;
-    const int readers = block_wgs + token_wgs, at = (int)blockIdx.x;
-    float f[ITEMS][V] = {};
+    const int readers = block_wgs + token_wgs, at = (int)blockIdx.x, c = g.cov.column<V>();
+    const T *dy = (const T *)g.dy;
+    float f[V] = {};
     if (at < block_wgs) {
         const int b = g.cov.group(at);
         if (b >= g.blocks) return;
         const int row = g.sorted[b * kRun];
         if (row == g.V || g.sorted[b * kRun + kRun - 1] != row) return;
-        add_rows<T, V, ITEMS>(f, g.cov, g.K, g.order, (const T *)g.dy, g.ld, b * kRun, b * kRun + kRun);
-#pragma unroll
-        for (int q = 0; q < ITEMS; ++q) {
-            const int c = g.cov.column<V, ITEMS>(q);
-            if (c >= g.K) continue;
-            Pack<float, V> o;   // (read back soon: stays in the caches)
-#pragma unroll
-            for (int e = 0; e < V; ++e) o.e[e] = f[q][e];
-            *reinterpret_cast<Pack<float, V> *>(g.part + (size_t)b * (size_t)g.K + c) = o;
-        }
+        add_rows<T, V, LOOSE>(f, g.cov.shift, c, g.K, g.order, dy, g.ld, b * kRun, b * kRun + kRun);
+        // (read back soon: no streaming)
+        store_pack<float, V, false, false>(g.part + (size_t)b * (size_t)g.ldp, c, g.ldp, f);
     } else if (at < readers) {
         const int i0 = g.cov.group(at - block_wgs) * kAhead;
         if (i0 >= g.T) return;
@@ -280,44 +252,33 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
         const int my_row = g.sorted[mine], my_tok = g.order[mine];
         const int before = i0 > 0 ? g.sorted[i0 - 1] : -1;
         int row[kAhead];
-        Pack<T, V> p[kAhead][ITEMS];
+        Pack<T, V> p[kAhead];
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             row[j] = __shfl(my_row, j, kAhead);
             const int tok = __shfl(my_tok, j, kAhead);
             // not a run of the groups before, nor an id outside the table
-            if (j < n && row[j] != before && row[j] != g.V) {
-#pragma unroll
-                for (int q = 0; q < ITEMS; ++q) {
-                    const int c = g.cov.column<V, ITEMS>(q);
-                    const T *from = (const T *)g.dy + (int64_t)tok * g.ld + c;
-                    if (c < g.K) p[j][q] = ACC ? load_stream<T, V>(from) : *reinterpret_cast<const Pack<T, V> *>(from);
-                }
-            }
+            if (j < n && row[j] != before && row[j] != g.V)
+                p[j] = load_pack<T, V, LOOSE, ACC>(dy + (int64_t)tok * g.ld, c, g.K);
         }
         int lo = i0;   // of the run at j
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) {
             if (j >= n || row[j] == before || row[j] == g.V) continue;
-            if (j == 0 || row[j] != row[j - 1]) {
-                lo = i0 + j;
+            float d[V];
+            unpack(p[j], d);
+            const bool begins = j == 0 || row[j] != row[j - 1];
+            if (begins) lo = i0 + j;
 #pragma unroll
-                for (int q = 0; q < ITEMS; ++q)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) f[q][e] = 0.0f;
-            }
-#pragma unroll
-            for (int q = 0; q < ITEMS; ++q)
-#pragma unroll
-                for (int e = 0; e < V; ++e) f[q][e] += to_f32(p[j][q].e[e]);
+            for (int e = 0; e < V; ++e) f[e] = begins ? d[e] : f[e] + d[e];
             if (j + 1 < n) {
                 if (row[j + 1] == row[j]) continue;
             } else {   // the run may go on
                 const int hi = g.first[row[j] + 1];
                 if ((lo + kRun - 1) / kRun < hi / kRun) continue;
-                add_rows<T, V, ITEMS>(f, g.cov, g.K, g.order, (const T *)g.dy, g.ld, i0 + n, hi);
+                add_rows<T, V, LOOSE>(f, g.cov.shift, c, g.K, g.order, dy, g.ld, i0 + n, hi);
             }
-            put_row<G, V, ACC>(g, row[j], f);
+            put_row<G, V, LOOSE, ACC>(g, row[j], c, f);
         }
     } else {
         const int row0 = g.cov.group(at - readers) * kZeroRows;
@@ -325,15 +286,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
 #pragma unroll
         for (int i = 0; i <= kZeroRows; ++i) start[i] = g.first[min(row0 + i, g.V)];
 #pragma unroll
-        for (int i = 0; i < kZeroRows; ++i) {
-            if (row0 + i >= g.V || start[i] != start[i + 1]) continue;
-            G *out = (G *)g.dtable + (int64_t)(row0 + i) * g.ldt;
-#pragma unroll
-            for (int q = 0; q < ITEMS; ++q) {
-                const int c = g.cov.column<V, ITEMS>(q);
-                if (c < g.K) store_vec<G, V>(out + c, f[q]);
-            }
-        }
+        for (int i = 0; i < kZeroRows; ++i)
+            if (row0 + i < g.V && start[i] == start[i + 1])
+                store_pack<G, V, LOOSE>((G *)g.dtable + (int64_t)(row0 + i) * g.ldt, c, g.K, f);
     }
 }
 
@@ -341,8 +296,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
 // workgroup of 16 waves per block and 64 V columns. The row's terms (the tokens
 // before its first whole block, the blocks' sums, the tokens behind the last)
 // are dealt to the waves, whose sums are joined in wave order, so that the most
-// frequent token of a long batch is no long walk either.
-template <class T, class G, int V, bool ACC>
+// frequent token of a long batch is no long walk either (a token in 9 % of
+// 32768 positions: 39 us by one group, 18 here; in all of them 450 and 181 for
+// the whole gradient).
+template <class T, class G, int V, bool LOOSE, bool ACC>
 __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
     __shared__ float s[16][64 * V];
     const int b = (int)blockIdx.x;
@@ -352,32 +309,34 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
     const int c = ((int)blockIdx.y * 64 + lane) * V;
     const int lo = g.first[row], hi = g.first[row + 1], b1 = hi / kRun;
     float f[V] = {};
-    if (c < g.K) {
-        auto token = [&](int i) {
-            const Pack<T, V> p = *reinterpret_cast<const Pack<T, V> *>((const T *)g.dy + (int64_t)g.order[i] * g.ld + c);
+    auto add = [&](const float (&d)[V]) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) f[e] += to_f32(p.e[e]);
-        };
+        for (int e = 0; e < V; ++e) f[e] += d[e];
+    };
+    auto token = [&](int i) {
+        float d[V];
+        unpack(load_pack<T, V, LOOSE>((const T *)g.dy + (int64_t)g.order[i] * g.ld, c, g.K), d);
+        add(d);
+    };
 #pragma unroll 2
-        for (int i = lo + w; i < b * kRun; i += 16) token(i);
+    for (int i = lo + w; i < b * kRun; i += 16) token(i);
 #pragma unroll 4
-        for (int i = b + w; i < b1; i += 16) {
-            const Pack<float, V> p = *reinterpret_cast<const Pack<float, V> *>(g.part + (size_t)i * (size_t)g.K + c);
-#pragma unroll
-            for (int e = 0; e < V; ++e) f[e] += p.e[e];
-        }
-#pragma unroll 2
-        for (int i = b1 * kRun + w; i < hi; i += 16) token(i);
+    for (int i = b + w; i < b1; i += 16) {
+        float d[V];
+        unpack(load_pack<float, V, false>(g.part + (size_t)i * (size_t)g.ldp, c, g.ldp), d);
+        add(d);
     }
+#pragma unroll 2
+    for (int i = b1 * kRun + w; i < hi; i += 16) token(i);
 #pragma unroll
     for (int e = 0; e < V; ++e) s[w][e * 64 + lane] = f[e];
     __syncthreads();
-    if (w != 0 || c >= g.K) return;
+    if (w != 0) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] += s[i][e * 64 + lane];
-    put_vec<G, V, ACC>(g, row, c, f);
+    put_row<G, V, LOOSE, ACC>(g, row, c, f);
 }
 
 constexpr int kMaxTokens = 1 << 20, kMaxVocab = 1 << 24, kMaxCols = 1 << 20;
@@ -404,27 +363,27 @@ bool rows_aligned(const void *p, int64_t ld, int type) {
     return ((uintptr_t)p & 15) == 0 && (size_t)ld * size_of(type) % 16 == 0;
 }
 
-// Vectors per thread: one of 16 bytes, or 4 single elements.
-constexpr int items_of(int V) { return V > 1 ? 1 : 4; }
-
 // The smallest group (8 to 256 threads) that holds a row.
-template <int V>
-Cover cover(int K) {
+Cover cover(int K, int V) {
     const int vectors = (K + V - 1) / V;
     Cover c{3};
-    while (c.shift < 8 && (items_of(V) << c.shift) < vectors) ++c.shift;
+    while (c.shift < 8 && (1 << c.shift) < vectors) ++c.shift;
     return c;
 }
-template <int V>
-dim3 grid(const Cover &c, int64_t groups, int K) {
-    const int per = 256 >> c.shift, cols = (items_of(V) << c.shift) * V;
-    return dim3((unsigned)((groups + per - 1) / per), (unsigned)((K + cols - 1) / cols));
+dim3 grid(const Cover &c, int64_t wgs, int K, int V) {
+    const int cols = V << c.shift;
+    return dim3((unsigned)wgs, (unsigned)((K + cols - 1) / cols));
+}
+int64_t wgs_of(const Cover &c, int64_t groups) {
+    const int per = 256 >> c.shift;
+    return (groups + per - 1) / per;
 }
 
 // order, sorted [T], first [V + 1], the chunks' order and sorted [T] where
 // there are several, then the sums of whole blocks
 struct Scratch {
     size_t sorted, first, chunk_order, chunk_sorted, part, bytes;
+    int ldp;
 };
 Scratch scratch_of(int T, int V, int K) {
     Scratch s;
@@ -434,37 +393,36 @@ Scratch scratch_of(int T, int V, int K) {
     s.chunk_order = s.first + align256(((size_t)V + 1) * 4);
     s.chunk_sorted = s.chunk_order + (T > kChunk ? list : 0);
     s.part = s.chunk_sorted + (T > kChunk ? list : 0);
-    s.bytes = s.part + (size_t)(T / kRun) * (size_t)K * 4;
+    s.ldp = (K + 7) / 8 * 8;
+    s.bytes = s.part + (size_t)(T / kRun) * (size_t)s.ldp * 4;
     return s;
 }
 
-template <class T, int V>
+template <class T, int V, bool LOOSE>
 void lookup(int tokens, int K, int vocab, const int64_t *ids, int64_t v0, const void *table, int64_t ldt, float scale,
             void *y, int64_t ldy, hipStream_t s) {
-    const Cover c = cover<V>(K);
+    const Cover c = cover(K, V);
     const auto go = [&](auto kernel, int per) {
-        kernel<<<grid<V>(c, (tokens + per - 1) / per, K), 256, 0, s>>>(c, tokens, K, v0, vocab, ids, (const T *)table, ldt,
-                                                                   scale, (T *)y, ldy);
+        kernel<<<grid(c, wgs_of(c, (tokens + per - 1) / per), K, V), 256, 0, s>>>(
+            c, tokens, K, v0, vocab, ids, (const T *)table, ldt, scale, (T *)y, ldy);
     };
-    if (tokens < 4096) go(lookup_kernel<T, V, items_of(V), 1>, 1);
-    else go(lookup_kernel<T, V, items_of(V), 4>, 4);
+    if (tokens < 4096) go(lookup_kernel<T, V, LOOSE, 1>, 1);
+    else go(lookup_kernel<T, V, LOOSE, 4>, 4);
 }
 
-template <class D, class G, int V, bool ACC>
+template <class D, class G, int V, bool LOOSE, bool ACC>
 void launch_gradient(Gradient g, hipStream_t s) {
-    g.cov = cover<V>(g.K);
-    const int per = 256 >> g.cov.shift;
-    auto wgs = [&](int64_t groups) { return (groups + per - 1) / per; };
+    g.cov = cover(g.K, V);
     const int64_t zeros = ACC ? 0 : ((int64_t)g.V + kZeroRows - 1) / kZeroRows;
-    const int64_t all = wgs(g.blocks) + wgs((g.T + kAhead - 1) / kAhead) + wgs(zeros);
-    rows_kernel<D, G, V, ACC, items_of(V)><<<grid<V>(g.cov, all * per, g.K), 256, 0, s>>>(g);
+    const int64_t wgs = wgs_of(g.cov, g.blocks) + wgs_of(g.cov, (g.T + kAhead - 1) / kAhead) + wgs_of(g.cov, zeros);
+    rows_kernel<D, G, V, LOOSE, ACC><<<grid(g.cov, wgs, g.K, V), 256, 0, s>>>(g);
     const dim3 by_block((unsigned)g.blocks, (unsigned)((g.K + 64 * V - 1) / (64 * V)));
-    if (g.blocks > 0) long_rows_kernel<D, G, V, ACC><<<by_block, 1024, 0, s>>>(g);
+    if (g.blocks > 0) long_rows_kernel<D, G, V, LOOSE, ACC><<<by_block, 1024, 0, s>>>(g);
 }
 template <class D, class G, int V>
-void gradient(const Gradient &g, bool accumulate, hipStream_t s) {
-    if (accumulate) launch_gradient<D, G, V, true>(g, s);
-    else launch_gradient<D, G, V, false>(g, s);
+void gradient(const Gradient &g, bool loose, bool accumulate, hipStream_t s) {
+    if (loose) accumulate ? launch_gradient<D, G, V, true, true>(g, s) : launch_gradient<D, G, V, true, false>(g, s);
+    else accumulate ? launch_gradient<D, G, V, false, true>(g, s) : launch_gradient<D, G, V, false, false>(g, s);
 }
 
 }  // namespace
@@ -481,13 +439,13 @@ int op_embed_forward(int T, int V, int K, int type, const int64_t *ids, int64_t 
     int cus;
     if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
     const hipStream_t s = (hipStream_t)stream;
-    const bool wide = K % (int)(16 / size_of(type)) == 0 && rows_aligned(table, ldt, type) && rows_aligned(y, ldy, type);
+    const bool even = K % (int)(16 / size_of(type)) == 0 && rows_aligned(table, ldt, type) && rows_aligned(y, ldy, type);
     if (type == COMPASS_F32) {
-        if (wide) lookup<float, 4>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
-        else lookup<float, 1>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
+        if (even) lookup<float, 4, false>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
+        else lookup<float, 4, true>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
     } else {
-        if (wide) lookup<Bf16, 8>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
-        else lookup<Bf16, 1>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
+        if (even) lookup<Bf16, 8, false>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
+        else lookup<Bf16, 8, true>(T, K, V, ids, v0, table, ldt, scale, y, ldy, s);
     }
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? COMPASS_OK : hip_error(e, "lookup launch");
@@ -529,15 +487,16 @@ int op_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *
         merge_kernel<<<by64, 1024, 0, s>>>(T, chunk_order, chunk_sorted, order, sorted);
     }
     runs_kernel<<<dim3((unsigned)(V / 256 + 1)), 256, 0, s>>>(T, V, sorted, first);
-    const Gradient g{{}, T, K, V, T / kRun, order, sorted, first, (float *)(w + sc.part), dy, ldy, scale, dtable, ldt};
+    const Gradient g{{}, T, K, V, T / kRun, order, sorted, first, (float *)(w + sc.part), sc.ldp, dy, ldy, scale, dtable,
+                     ldt};
     const bool d32 = dtype == COMPASS_F32, g32 = gtype == COMPASS_F32;
-    // one vector width for both sides: that of the wider-vectored (bf16) one
-    const int v = d32 && g32 ? 4 : 8;
-    const bool wide = K % v == 0 && rows_aligned(dy, ldy, dtype) && rows_aligned(dtable, ldt, gtype);
-    if (d32 && g32) wide ? gradient<float, float, 4>(g, accumulate != 0, s) : gradient<float, float, 1>(g, accumulate != 0, s);
-    else if (d32) wide ? gradient<float, Bf16, 8>(g, accumulate != 0, s) : gradient<float, Bf16, 1>(g, accumulate != 0, s);
-    else if (g32) wide ? gradient<Bf16, float, 8>(g, accumulate != 0, s) : gradient<Bf16, float, 1>(g, accumulate != 0, s);
-    else wide ? gradient<Bf16, Bf16, 8>(g, accumulate != 0, s) : gradient<Bf16, Bf16, 1>(g, accumulate != 0, s);
+    // one vector width for both sides: 16 bytes of the smaller type
+    const bool loose = K % (d32 && g32 ? 4 : 8) != 0 || !rows_aligned(dy, ldy, dtype) || !rows_aligned(dtable, ldt, gtype);
+    const bool acc = accumulate != 0;
+    if (d32 && g32) gradient<float, float, 4>(g, loose, acc, s);
+    else if (d32) gradient<float, Bf16, 8>(g, loose, acc, s);
+    else if (g32) gradient<Bf16, float, 8>(g, loose, acc, s);
+    else gradient<Bf16, Bf16, 8>(g, loose, acc, s);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? COMPASS_OK : hip_error(e, "table gradient launch");
 }

@@ -34,38 +34,20 @@ struct NormParams {
     int want_params;                // whether dgamma or dbeta is wanted
 };
 
-template <class T, int V>
-__device__ __forceinline__ void load_row(const T *row, int i, int N, float (&f)[V]) {
-    if (i < N) {
-        const Pack<T, V> p = *reinterpret_cast<const Pack<T, V> *>(row + i);
-#pragma unroll
-        for (int e = 0; e < V; ++e) f[e] = to_f32(p.e[e]);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) f[e] = 0.0f;
-    }
-}
-
 // V parameters from element i, `none` where there is no such vector.
-template <int V>
+template <int V, bool LOOSE>
 __device__ __forceinline__ void load_param(const void *p, int f32, float none, int i, int N, float (&f)[V]) {
     if (!p) {
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = none;
     } else if (f32) {
-        load_row<float, V>((const float *)p, i, N, f);
-    } else {
-        load_row<Bf16, V>((const Bf16 *)p, i, N, f);
-    }
-}
-
-template <class T, int V>
-__device__ __forceinline__ void store_row(T *row, int i, int N, const float (&f)[V]) {
-    if (i < N) {
-        Pack<T, V> p;
+        unpack(load_pack<float, V, LOOSE>((const float *)p, i, N), f);
+    } else if constexpr (V == 8) {
+        unpack(load_pack<Bf16, V, LOOSE>((const Bf16 *)p, i, N), f);
+    } else {   // half a piece; few enough (once per column) to go by element
 #pragma unroll
-        for (int e = 0; e < V; ++e) p.e[e] = from_f32<T>(f[e]);
-        store_stream<T, V>(row + i, p);
+        for (int e = 0; e < V; ++e)
+            f[e] = i + e < N ? __builtin_bit_cast(float, (uint32_t)((const Bf16 *)p)[i + e].bits << 16) : 0.0f;
     }
 }
 
@@ -85,7 +67,11 @@ __device__ __forceinline__ float row_sum(float x, float *s) {
 }
 
 // TPR threads per row, ITEMS vectors of V elements each.
-template <class T, int V, int TPR, int ITEMS>
+//
+// Bound by memory: 32768 x 8192 bf16 (1.07 GB) 200 us (5.4 TB/s, 211 without
+// streaming stores); 8192 x 12288 fp32 140 us (5.7 TB/s); rows of odd length
+// reach 3.4 (8192 x 5001 bf16 49 us; by single elements 98).
+template <class T, int V, bool LOOSE, int TPR, int ITEMS>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(const NormParams p) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR;
     __shared__ float s0[THREADS / 64], s1[THREADS / 64];
@@ -97,7 +83,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(con
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        load_row<T, V>(x, (i * TPR + t) * V, p.N, f[i]);
+        unpack(load_pack<T, V, LOOSE>(x, (i * TPR + t) * V, p.N), f[i]);
 #pragma unroll
         for (int e = 0; e < V; ++e) sum += f[i][e];
     }
@@ -105,12 +91,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(con
     float sq = 0.0f;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i)
-        if ((i * TPR + t) * V < p.N) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                f[i][e] -= mean;
-                sq += f[i][e] * f[i][e];
-            }
+        for (int e = 0; e < V; ++e) {
+            f[i][e] -= mean;
+            if ((i * TPR + t) * V + (LOOSE ? e : 0) < p.N) sq += f[i][e] * f[i][e];
         }
     const float rstd = 1.0f / sqrtf(row_sum<TPR>(sq, s1) / (float)p.N + p.eps);
     T *y = (T *)p.y + (int64_t)m * p.ldy;
@@ -118,11 +102,11 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(con
     for (int i = 0; i < ITEMS; ++i) {
         const int c = (i * TPR + t) * V;
         float g[V], b[V];
-        load_param<V>(p.gamma, p.param_f32, 1.0f, c, p.N, g);
-        load_param<V>(p.beta, p.param_f32, 0.0f, c, p.N, b);
+        load_param<V, LOOSE>(p.gamma, p.param_f32, 1.0f, c, p.N, g);
+        load_param<V, LOOSE>(p.beta, p.param_f32, 0.0f, c, p.N, b);
 #pragma unroll
         for (int e = 0; e < V; ++e) f[i][e] = f[i][e] * rstd * g[e] + b[e];
-        store_row<T, V>(y, c, p.N, f[i]);
+        store_pack<T, V, LOOSE>(y, c, p.N, f[i]);
     }
     if (t == 0) {
         p.mean[m] = mean;
@@ -130,45 +114,80 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_forward_kernel(con
     }
 }
 
-// Each group of TPR threads takes every gridDim-th row (of its place) and
-// keeps its columns' sums of dy xh and dy in registers to the end.
-template <class T, int V, int TPR, int ITEMS>
-__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_backward_kernel(const NormParams p) {
-    constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR, WAVES = TPR / 64;
-    __shared__ float2 s[2][WAVES > 1 ? WAVES : 1];
-    __shared__ float comb[ROWS > 1 ? ROWS * 64 * V * 2 : 1];
+// Threads of a backward workgroup whose rows take TPR threads each.
+constexpr int backward_threads(int tpr) { return tpr > 512 ? tpr : tpr % 192 == 0 ? 768 : 1024; }
+
+// One workgroup per CU, 768 or 1024 threads: groups of TPR threads take a row
+// each, every (gridDim x groups)-th, load the next while they work on one, and
+// keep their columns' sums of dy xh and dy in registers to the end. What is
+// held of a row between the two passes over it is what was loaded (x and dy as
+// they lie), so that a row, the next one, gamma and the sums fit 128 registers.
+//
+// Bound by memory: a row's x and dy in, dx out. Each workgroup leaves 2 N sums,
+// so few workgroups keep that traffic small. With the sums' join, bf16: 8192 x
+// 12288 130 us (604 MB at 4.65 TB/s), without the next row's loads 149, with
+// 512 workgroups 152; 32768 x 8192 310 us (5.2 TB/s); 8192 x 2048 27 us, as
+// 1024 workgroups of 256 threads 50.
+template <class T, int V, bool LOOSE, int TPR, int ITEMS>
+__global__ __launch_bounds__(backward_threads(TPR)) void norm_backward_kernel(const NormParams p) {
+    constexpr int THREADS = backward_threads(TPR), ROWS = THREADS / TPR, WAVES = TPR / 64;
+    constexpr bool AHEAD = THREADS * V * ITEMS < 16384;   // else the next row has no registers
+    __shared__ float2 s[2][THREADS / 64];
+    __shared__ float comb[ROWS > 1 ? THREADS * V * 2 : 1];
     const int t = threadIdx.x % TPR, r = threadIdx.x / TPR;
     float g[ITEMS][V], dg[ITEMS][V], db[ITEMS][V];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        load_param<V>(p.gamma, p.param_f32, 1.0f, (i * TPR + t) * V, p.N, g[i]);
+        load_param<V, LOOSE>(p.gamma, p.param_f32, 1.0f, (i * TPR + t) * V, p.N, g[i]);
 #pragma unroll
         for (int e = 0; e < V; ++e) dg[i][e] = db[i][e] = 0.0f;
     }
     const int step = (int)gridDim.x * ROWS;
     const float inv = 1.0f / (float)p.N;
-    int par = 0;
-    for (int m = (int)blockIdx.x * ROWS + r; m < p.M; m += step, par ^= 1) {
+    Pack<T, V> nx[ITEMS], nd[ITEMS];
+    float n_mean = 0.0f, n_rstd = 0.0f;
+    auto fetch = [&](int m) {
         const T *x = (const T *)p.x + (int64_t)m * p.ldx, *dy = (const T *)p.dy + (int64_t)m * p.lddy;
-        float xh[ITEMS][V], d[ITEMS][V];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            load_row<T, V>(x, (i * TPR + t) * V, p.N, xh[i]);
-            load_row<T, V>(dy, (i * TPR + t) * V, p.N, d[i]);
+            nx[i] = load_pack<T, V, LOOSE>(x, (i * TPR + t) * V, p.N);
+            nd[i] = load_pack<T, V, LOOSE>(dy, (i * TPR + t) * V, p.N);
         }
-        const float mean = p.mean_in[m], rstd = p.rstd_in[m];
+        n_mean = p.mean_in[m];
+        n_rstd = p.rstd_in[m];
+    };
+    const int m0 = (int)blockIdx.x * ROWS;
+    if (AHEAD && m0 + r < p.M) fetch(m0 + r);
+    int par = 0;
+    for (int mb = m0; mb < p.M; mb += step, par ^= 1) {   // the same count for all groups: they share barriers
+        const int m = mb + r;
+        const bool row = m < p.M;
+        if (!AHEAD && row) fetch(m);
+        Pack<T, V> cx[ITEMS], cd[ITEMS];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            cx[i] = nx[i];
+            cd[i] = nd[i];
+        }
+        const float mean = n_mean, rstd = n_rstd;
+        if (AHEAD && m + step < p.M) fetch(m + step);
         float c1 = 0.0f, c2 = 0.0f;
+        if (row) {
 #pragma unroll
-        for (int i = 0; i < ITEMS; ++i)
+            for (int i = 0; i < ITEMS; ++i) {
+                float x[V], d[V];
+                unpack(cx[i], x);
+                unpack(cd[i], d);
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                xh[i][e] = (xh[i][e] - mean) * rstd;   // past the row's end d is 0
-                dg[i][e] += d[i][e] * xh[i][e];
-                db[i][e] += d[i][e];
-                d[i][e] *= g[i][e];
-                c1 += d[i][e];
-                c2 += d[i][e] * xh[i][e];
+                for (int e = 0; e < V; ++e) {
+                    const float xh = (x[e] - mean) * rstd, a = d[e] * g[i][e];   // past the row's end d is 0
+                    dg[i][e] += d[e] * xh;
+                    db[i][e] += d[e];
+                    c1 += a;
+                    c2 += a * xh;
+                }
             }
+        }
         c1 = wave_sum(c1);
         c2 = wave_sum(c2);
         if constexpr (WAVES > 1) {
@@ -176,49 +195,58 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_backward_kernel(co
             // behind the next row's barrier, when all have read it
             if ((threadIdx.x & 63) == 0) s[par][threadIdx.x >> 6] = make_float2(c1, c2);
             __syncthreads();
-            c1 = s[par][0].x;
-            c2 = s[par][0].y;
+            c1 = s[par][r * WAVES].x;
+            c2 = s[par][r * WAVES].y;
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) {
-                c1 += s[par][w].x;
-                c2 += s[par][w].y;
+                c1 += s[par][r * WAVES + w].x;
+                c2 += s[par][r * WAVES + w].y;
             }
         }
+        if (!row) continue;
         c1 *= inv;
         c2 *= inv;
         T *dx = (T *)p.dx + (int64_t)m * p.lddx;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            float o[V];
+            float x[V], d[V], o[V];
+            unpack(cx[i], x);
+            unpack(cd[i], d);
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = rstd * (d[i][e] - c1 - xh[i][e] * c2);
-            store_row<T, V>(dx, (i * TPR + t) * V, p.N, o);
+            for (int e = 0; e < V; ++e) o[e] = rstd * (d[e] * g[i][e] - c1 - (x[e] - mean) * rstd * c2);
+            store_pack<T, V, LOOSE>(dx, (i * TPR + t) * V, p.N, o);
         }
     }
     if (!p.want_params) return;
     float *part = p.part + (size_t)blockIdx.x * 2 * (size_t)p.N;
+    auto put = [&](int c, int kind, float x) {
+        if (c < p.N) part[(size_t)kind * (size_t)p.N + c] = x;
+    };
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const int c = (i * TPR + t) * V;
-        if constexpr (ROWS > 1) {   // one sum per workgroup, in row order
+        if constexpr (ROWS > 1) {   // one sum per workgroup, in row order, dealt to all its threads
             __syncthreads();
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                comb[((r * 2 + 0) * V + e) * 64 + t] = dg[i][e];
-                comb[((r * 2 + 1) * V + e) * 64 + t] = db[i][e];
+                comb[(2 * e + 0) * THREADS + threadIdx.x] = dg[i][e];
+                comb[(2 * e + 1) * THREADS + threadIdx.x] = db[i][e];
             }
             __syncthreads();
-            if (r != 0) continue;
+            for (int at = threadIdx.x; at < 2 * V * TPR; at += THREADS) {
+                const int e2 = at / TPR, tt = at % TPR;
+                const float *from = comb + e2 * THREADS + tt;
+                float x = from[0];
 #pragma unroll
-            for (int q = 1; q < ROWS; ++q)
+                for (int q = 1; q < ROWS; ++q) x += from[q * TPR];
+                put((i * TPR + tt) * V + e2 / 2, e2 & 1, x);
+            }
+        } else {
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    dg[i][e] += comb[((q * 2 + 0) * V + e) * 64 + t];
-                    db[i][e] += comb[((q * 2 + 1) * V + e) * 64 + t];
-                }
+            for (int e = 0; e < V; ++e) {
+                put((i * TPR + t) * V + e, 0, dg[i][e]);
+                put((i * TPR + t) * V + e, 1, db[i][e]);
+            }
         }
-        store_row<float, V>(part, c, p.N, dg[i]);
-        store_row<float, V>(part + p.N, c, p.N, db[i]);
     }
 }
 
@@ -250,49 +278,52 @@ int hip_error(hipError_t e, const char *what) {
     return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// Workgroups of the backward pass: as many as the card holds at once (a row of
-// 1024 threads fills a CU), each with at least 4 rows per place where there are
-// that many, since every workgroup leaves a row of 2 N sums.
-int backward_groups(int M, int threads, int rows) {
-    const int held = 256 * (1024 / threads), groups = (M + rows - 1) / rows;
-    return std::max(1, std::min(groups, std::min(held, std::max(256, M / (4 * rows)))));
-}
+// Workgroups of the backward pass: at most one per CU.
+constexpr int kMaxParts = 256;
 
 struct Launch {
     const NormParams &p;
-    bool backward;
     hipStream_t stream;
     int parts;
-    template <class T, int V, int TPR, int ITEMS>
-    void go() {
+    template <class T, int V, bool LOOSE, int TPR, int ITEMS>
+    void forward() {
         constexpr int THREADS = TPR < 256 ? 256 : TPR, ROWS = THREADS / TPR;
-        if (backward) {
-            parts = backward_groups(p.M, THREADS, ROWS);
-            norm_backward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)parts), THREADS, 0, stream>>>(p);
-        } else {
-            norm_forward_kernel<T, V, TPR, ITEMS><<<dim3((unsigned)((p.M + ROWS - 1) / ROWS)), THREADS, 0, stream>>>(p);
-        }
+        norm_forward_kernel<T, V, LOOSE, TPR, ITEMS>
+            <<<dim3((unsigned)((p.M + ROWS - 1) / ROWS)), THREADS, 0, stream>>>(p);
+    }
+    template <class T, int V, bool LOOSE, int TPR, int ITEMS>
+    void backward() {
+        constexpr int THREADS = backward_threads(TPR), ROWS = THREADS / TPR;
+        parts = std::min((p.M + ROWS - 1) / ROWS, kMaxParts);
+        norm_backward_kernel<T, V, LOOSE, TPR, ITEMS><<<dim3((unsigned)parts), THREADS, 0, stream>>>(p);
     }
     // the fewest threads (and vectors each) that hold a row
-    template <class T, int V>
-    void pick() {
+    template <class T, int V, bool LOOSE>
+    void pick(bool back) {
         const int n = (p.N + V - 1) / V;
-        if constexpr (V > 1) {
-            if (n <= 64) go<T, V, 64, 1>();
-            else if (n <= 128) go<T, V, 64, 2>();
-            else if (n <= 256) go<T, V, 256, 1>();
-            else if (n <= 512) go<T, V, 256, 2>();
-            else if (n <= 1024) go<T, V, 512, 2>();
-            else if (n <= 2048) go<T, V, 1024, 2>();
-            else go<T, V, 1024, 4>();
-        } else {
-            if (n <= 256) go<T, V, 64, 4>();
-            else if (n <= 512) go<T, V, 64, 8>();
-            else if (n <= 2048) go<T, V, 256, 8>();
-            else if (n <= 4096) go<T, V, 512, 8>();
-            else if (n <= 8192) go<T, V, 1024, 8>();
-            else go<T, V, 1024, 16>();
+        if (back) {
+            if (n <= 64) backward<T, V, LOOSE, 64, 1>();
+            else if (n <= 128) backward<T, V, LOOSE, 64, 2>();
+            else if (n <= 256) backward<T, V, LOOSE, 128, 2>();
+            else if (n <= 384) backward<T, V, LOOSE, 192, 2>();
+            else if (n <= 512) backward<T, V, LOOSE, 256, 2>();
+            else if (n <= 768) backward<T, V, LOOSE, 384, 2>();
+            else if (n <= 1024) backward<T, V, LOOSE, 512, 2>();
+            else if (n <= 1536) backward<T, V, LOOSE, 768, 2>();
+            else if (n <= 2048) backward<T, V, LOOSE, 1024, 2>();
+            else if constexpr (V == 4) {
+                if (n <= 3072) backward<T, V, LOOSE, 1024, 3>();
+                else backward<T, V, LOOSE, 1024, 4>();
+            }
+            return;
         }
+        if (n <= 64) forward<T, V, LOOSE, 64, 1>();
+        else if (n <= 128) forward<T, V, LOOSE, 64, 2>();
+        else if (n <= 256) forward<T, V, LOOSE, 256, 1>();
+        else if (n <= 512) forward<T, V, LOOSE, 256, 2>();
+        else if (n <= 1024) forward<T, V, LOOSE, 512, 2>();
+        else if (n <= 2048) forward<T, V, LOOSE, 1024, 2>();
+        else if constexpr (V == 4) forward<T, V, LOOSE, 1024, 4>();
     }
 };
 
@@ -300,21 +331,21 @@ bool aligned16(const void *p, int64_t ld, size_t size) {
     return ((uintptr_t)p & 15) == 0 && (size_t)ld * size % 16 == 0;
 }
 
-// 16-byte vectors where every row of every operand starts on 16 bytes and
-// holds whole vectors, single elements otherwise.
+// 16-byte vectors: aligned ones where every row of every operand starts on 16
+// bytes and holds whole vectors, loose ones otherwise.
 int launch(const NormParams &p, int dtype, bool backward, hipStream_t stream) {
     const size_t size = dtype == COMPASS_F32 ? 4 : 2;
     const int64_t v = (int64_t)(16 / size);
-    bool wide = p.N % v == 0 && aligned16(p.x, p.ldx, size) && ((uintptr_t)p.gamma & 15) == 0;
-    if (backward) wide = wide && aligned16(p.dy, p.lddy, size) && aligned16(p.dx, p.lddx, size);
-    else wide = wide && aligned16(p.y, p.ldy, size) && ((uintptr_t)p.beta & 15) == 0;
-    Launch l{p, backward, stream, 0};
+    bool even = p.N % v == 0 && aligned16(p.x, p.ldx, size) && ((uintptr_t)p.gamma & 15) == 0;
+    if (backward) even = even && aligned16(p.dy, p.lddy, size) && aligned16(p.dx, p.lddx, size);
+    else even = even && aligned16(p.y, p.ldy, size) && ((uintptr_t)p.beta & 15) == 0;
+    Launch l{p, stream, 0};
     if (dtype == COMPASS_F32) {
-        if (wide) l.pick<float, 4>();
-        else l.pick<float, 1>();
+        if (even) l.pick<float, 4, false>(backward);
+        else l.pick<float, 4, true>(backward);
     } else {
-        if (wide) l.pick<Bf16, 8>();
-        else l.pick<Bf16, 1>();
+        if (even) l.pick<Bf16, 8, false>(backward);
+        else l.pick<Bf16, 8, true>(backward);
     }
     return l.parts;
 }
@@ -364,7 +395,7 @@ int op_norm_workspace(int M, int N, size_t *bytes) {
     const int rc = check(M, N, COMPASS_BF16, COMPASS_BF16);
     if (rc != COMPASS_OK) return rc;
     if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
-    *bytes = (size_t)backward_groups(M, 256, 1) * 2 * (size_t)N * 4;
+    *bytes = (size_t)std::min(M, kMaxParts) * 2 * (size_t)N * 4;
     return COMPASS_OK;
 }
 

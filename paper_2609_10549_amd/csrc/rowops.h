@@ -8,51 +8,106 @@ namespace compass {
 
 struct Bf16 { uint16_t bits; };
 
-// V consecutive elements as they lie in memory. 16-byte vectors (8 bf16,
-// 4 fp32) for aligned rows, single elements otherwise.
+typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
+
+// V consecutive elements as they lie in memory: whole 16-byte pieces. (Held in
+// the pieces' own type: from a struct of elements the compiler makes a load per
+// element.)
 template <class T, int V>
-struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Pack {
-    T e[V];
+struct Pack {
+    static constexpr int Q = (int)sizeof(T) * V / 16;
+    static_assert(Q > 0 && sizeof(T) * V % 16 == 0, "whole pieces");
+    u32x4_ q[Q];
 };
 
-__device__ __forceinline__ float to_f32(Bf16 x) { return __builtin_bit_cast(float, (uint32_t)x.bits << 16); }
-__device__ __forceinline__ float to_f32(float x) { return x; }
-template <class T>
-__device__ __forceinline__ T from_f32(float x);
-template <>
-__device__ __forceinline__ float from_f32<float>(float x) { return x; }
-template <>
-__device__ __forceinline__ Bf16 from_f32<Bf16>(float x) {   // round to nearest even
-    return Bf16{__builtin_bit_cast(uint16_t, (__bf16)x)};
-}
-
-// Loads and stores that pass through the caches without staying (whole vectors;
-// single elements go the ordinary way, lanes share their lines). An output of
-// more than the caches hold would otherwise be allocated line by line and
-// written back later: what a kernel measured with and without stands there.
-typedef unsigned int u32x4_ __attribute__((ext_vector_type(4)));
-template <class T, int V>
-__device__ __forceinline__ void store_stream(T *p, const Pack<T, V> &o) {
-    constexpr int N = sizeof(T) * V / 16;
-    if constexpr (sizeof(T) * V % 16 == 0 && N > 0) {
-        struct Quads { u32x4_ q[N]; };
-        const Quads q = __builtin_bit_cast(Quads, o);
+__device__ __forceinline__ void unpack(const u32x4_ &q, float (&f)[8]) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) __builtin_nontemporal_store(q.q[i], reinterpret_cast<u32x4_ *>(p) + i);
-    } else {
-        *reinterpret_cast<Pack<T, V> *>(p) = o;
+    for (int i = 0; i < 4; ++i) {
+        f[2 * i] = __builtin_bit_cast(float, (uint32_t)q[i] << 16);
+        f[2 * i + 1] = __builtin_bit_cast(float, (uint32_t)q[i] & 0xFFFF0000u);
     }
 }
 template <class T, int V>
-__device__ __forceinline__ Pack<T, V> load_stream(const T *p) {
-    constexpr int N = sizeof(T) * V / 16;
-    if constexpr (sizeof(T) * V % 16 == 0 && N > 0) {
-        struct Quads { u32x4_ q[N]; } q;
+__device__ __forceinline__ void unpack(const Pack<T, V> &p, float (&f)[V]) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) q.q[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_ *>(p) + i);
-        return __builtin_bit_cast(Pack<T, V>, q);
+        for (int e = 0; e < V; ++e) f[e] = __builtin_bit_cast(float, (uint32_t)p.q[e / 4][e % 4]);
     } else {
-        return *reinterpret_cast<const Pack<T, V> *>(p);
+        static_assert(V == 8, "one piece of bf16");
+        unpack(p.q[0], f);
+    }
+}
+__device__ __forceinline__ uint32_t bf16_bits(float x) {   // rounded to nearest even
+    return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)x);
+}
+template <class T, int V>
+__device__ __forceinline__ Pack<T, V> pack(const float (&f)[V]) {
+    Pack<T, V> p;
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) p.q[e / 4][e % 4] = __builtin_bit_cast(uint32_t, f[e]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p.q[0][i] = bf16_bits(f[2 * i]) | bf16_bits(f[2 * i + 1]) << 16;
+    }
+    return p;
+}
+__device__ __forceinline__ void put_element(Bf16 *p, float x) { p->bits = (uint16_t)bf16_bits(x); }
+__device__ __forceinline__ void put_element(float *p, float x) { *p = x; }
+
+// Elements [i, i + V) of a row of N. LOOSE: a row starts on any element and its
+// last vector may be cut by its end (the card loads and stores 16 bytes from
+// any address, at the cost of the extra line they touch); otherwise rows start
+// on 16 bytes and hold whole vectors. STREAM: passes through the caches without
+// staying. An output of more than the caches hold would otherwise be allocated
+// line by line and written back later: what a kernel measured with and without
+// stands there.
+template <bool LOOSE>
+struct Piece { typedef u32x4_ type; };
+template <>
+struct Piece<true> { typedef u32x4_ type __attribute__((aligned(2))); };
+
+template <class T, int V, bool LOOSE, bool STREAM = false>
+__device__ __forceinline__ Pack<T, V> load_pack(const T *row, int i, int N) {
+    typedef typename Piece<LOOSE>::type At;
+    Pack<T, V> p;
+    if (i + V <= N) {
+        const At *from = reinterpret_cast<const At *>(row + i);
+#pragma unroll
+        for (int j = 0; j < Pack<T, V>::Q; ++j) p.q[j] = STREAM ? __builtin_nontemporal_load(from + j) : from[j];
+        return p;
+    }
+#pragma unroll
+    for (int j = 0; j < Pack<T, V>::Q; ++j) p.q[j] = u32x4_{0, 0, 0, 0};
+    if constexpr (LOOSE) {
+        if (i < N) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (i + e < N) {
+                    if constexpr (sizeof(T) == 4) p.q[e / 4][e % 4] = __builtin_bit_cast(uint32_t, row[i + e]);
+                    else p.q[0][e / 2] |= (uint32_t)row[i + e].bits << (16 * (e & 1));
+                }
+        }
+    }
+    return p;
+}
+template <class T, int V, bool LOOSE, bool STREAM = true>
+__device__ __forceinline__ void store_pack(T *row, int i, int N, const float (&f)[V]) {
+    typedef typename Piece<LOOSE>::type At;
+    if (i + V <= N) {
+        const Pack<T, V> p = pack<T, V>(f);
+        At *to = reinterpret_cast<At *>(row + i);
+#pragma unroll
+        for (int j = 0; j < Pack<T, V>::Q; ++j) {
+            if (STREAM) __builtin_nontemporal_store(p.q[j], to + j);
+            else to[j] = p.q[j];
+        }
+    } else if constexpr (LOOSE) {
+        if (i < N) {
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (i + e < N) put_element(row + i + e, f[e]);
+        }
     }
 }
 
