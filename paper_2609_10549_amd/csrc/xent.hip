@@ -36,7 +36,7 @@ namespace {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 enum Epilogue : int {
     kStats = 0,   // row maxima and sums of exponentials, the targets' logits
@@ -206,19 +206,33 @@ __device__ __forceinline__ void mfma_run(f32x4 (&acc)[FN][FM], const bf16x8 (&a)
     }
 }
 
-__device__ __forceinline__ float wave16_max(float x) {   // over the four lanes of a row
-    x = fmaxf(x, __shfl_xor(x, 16));
-    return fmaxf(x, __shfl_xor(x, 32));
+// Over the four lanes that hold a row: the wave's 16-lane rows exchanged.
+__device__ __forceinline__ void row_pairs(float x, bool far, float *a, float *b) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, x);
+    const u32x2 r = far ? __builtin_amdgcn_permlane32_swap(u, u, false, false)
+                        : __builtin_amdgcn_permlane16_swap(u, u, false, false);
+    *a = __builtin_bit_cast(float, (uint32_t)r[0]);
+    *b = __builtin_bit_cast(float, (uint32_t)r[1]);
 }
-__device__ __forceinline__ float wave16_sum(float x) {
-    x += __shfl_xor(x, 16);
-    return x + __shfl_xor(x, 32);
+__device__ __forceinline__ float row_max(float x) {
+    float a, b;
+    row_pairs(x, false, &a, &b);
+    row_pairs(fmaxf(a, b), true, &a, &b);
+    return fmaxf(a, b);
+}
+__device__ __forceinline__ float row_sum(float x) {
+    float a, b;
+    row_pairs(x, false, &a, &b);
+    row_pairs(a + b, true, &a, &b);
+    return a + b;
 }
 
-// One BM x BN tile per workgroup; 4 waves, 2 x 2 over the tile. The main loop
-// (stages of 64, DW + 1 buffers of A and DW of B, counted waits, one barrier
-// per stage, LDS reads and loads one at a time between the MFMAs) is
-// gemm_kernel's; see there for what each part of it is worth.
+// BM x BN tiles, 4 waves, 2 x 2 over the tile. The main loop (stages of 64,
+// DW + 1 buffers of A and DW of B, counted waits, one barrier per stage, LDS
+// reads and loads one at a time between the MFMAs) is gemm_kernel's; see there
+// for what each part of it is worth. A workgroup takes a tile of every round;
+// with kPre the next tile's first stages are on their way while the epilogue
+// runs (the epilogue's LDS is then the buffer that those stages leave free).
 template <int BM, int BN, int DW, bool AT, bool BT, int EPI>
 __global__ __launch_bounds__(kThreads, (160 << 10) / (((DW + 1) * BM + DW * BN) * 128))
 void tile_kernel(const TileParams p) {
@@ -228,174 +242,219 @@ void tile_kernel(const TileParams p) {
     constexpr int SA = BM * 128, SW = BN * 128;
     constexpr int NA = DW + 1;
     constexpr bool kAcc = NA * SA + DW * SW > (80 << 10);   // one workgroup per CU
+    constexpr int kRegion = EPI == kStats ? 0 : FN * (EPI == kPart ? 2048 : 1024);   // bytes per wave, 32 rows
+    constexpr bool kPre = 4 * kRegion <= SA;
     __shared__ __attribute__((aligned(1024))) char smem[NA * SA + DW * SW];
+    static_assert(4 * kRegion <= NA * SA + DW * SW, "the epilogue regions fit");
 
     const int tid = threadIdx.x;
     const int lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm0 = (wave >> 1) * WM, wn0 = (wave & 1) * WN;
+    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.slices, grid = (int)gridDim.x;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(smem);
+    const uint32_t ldsW = lds0 + NA * SA, ldsE = ldsW + DW * SW;
 
-    // consecutive positions to one XCD (workgroups go round-robin over the 8
-    // XCDs), group_m row tiles before the next column tile: the tiles an XCD
-    // holds at a time share rows of A and columns of B in its L2
-    const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.slices;
-    const int v = (int)blockIdx.x & 7, c = (int)blockIdx.x >> 3;
-    const int pos = v * (total >> 3) + min(v, total & 7) + c;
-    const int slice = pos / tiles, tpos = pos - slice * tiles;
-    const int gsz = p.group_m * p.tiles_n;
-    const int grp = tpos / gsz, rin = tpos - grp * gsz;
-    const int rows_here = min(p.group_m, p.tiles_m - grp * p.group_m);
-    const int tm = grp * p.group_m + rin % rows_here, tn = rin / rows_here;
-    const int m0 = p.m_base + tm * BM, n0 = p.n_base + tn * BN;
-    const int kb = slice * p.kslice, ke = min(p.R, kb + p.kslice);
+    // Tile of this workgroup in round j, false when there is none. Each XCD
+    // (workgroups go round-robin over them) walks a run of its own, an eighth of
+    // the positions, which go down group_m row tiles before the next column
+    // tile: what it holds at a time shares rows and columns in its L2, and the
+    // XCDs, at different rows, go over the same columns together.
+    struct Tile { int m0, n0, tn, slice, kb, ke; };
+    auto tile_of_round = [&](int j, Tile &t) {
+        const int v = (int)blockIdx.x & 7, c = (int)blockIdx.x >> 3;
+        const int at = j * ((grid >> 3) + (v < (grid & 7) ? 1 : 0)) + c;
+        if (at >= (total >> 3) + (v < (total & 7) ? 1 : 0)) return false;
+        const int pos = v * (total >> 3) + min(v, total & 7) + at;
+        t.slice = pos / tiles;
+        const int tpos = pos - t.slice * tiles, gsz = p.group_m * p.tiles_n;
+        const int grp = tpos / gsz, rin = tpos - grp * gsz;
+        const int rows_here = min(p.group_m, p.tiles_m - grp * p.group_m);
+        t.tn = rin / rows_here;
+        t.m0 = p.m_base + (grp * p.group_m + rin - t.tn * rows_here) * BM;
+        t.n0 = p.n_base + t.tn * BN;
+        t.kb = t.slice * p.kslice;
+        t.ke = min(p.R, t.kb + p.kslice);
+        return true;
+    };
 
-    f32x4 acc[FN][FM];
-#pragma unroll
-    for (int ni = 0; ni < FN; ++ni)
-#pragma unroll
-        for (int mi = 0; mi < FM; ++mi) acc[ni][mi] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-    {
-        Loader<AT, BM> la;
-        Loader<BT, BN> lb;
-        la.init(p.A, p.a_bytes, m0, p.M, p.lda, kb, ke, lane, wave);
-        lb.init(p.B, p.b_bytes, n0, p.N, p.ldb, kb, ke, lane, wave);
-        Reader<AT, BM, FM> ra;
-        Reader<BT, BN, FN> rb;
-        ra.init(wm0, lane);
-        rb.init(wn0, lane);
-        const int KT = (ke - kb + kBK - 1) / kBK;
-        const uint32_t lds0 = (uint32_t)(uintptr_t)LDS_AS(smem);
-        const uint32_t ldsW = lds0 + NA * SA, ldsE = ldsW + DW * SW;
-        const uint32_t wb = (uint32_t)wave * 1024u;
-        i32x4 sA, sB;
+    Loader<AT, BM> la;
+    Loader<BT, BN> lb;
+    // The lane's number, not known to the compiler to be the same at every call:
+    // what is derived from it is computed where it is needed, not kept in
+    // registers (and spilled) from one tile to the next.
+    auto fresh_lane = [&]() {
+        int l = lane;
+        asm volatile("" : "+v"(l));
+        return l;
+    };
+    auto begin = [&](const Tile &t) {   // the tile's first DW stages
+        const int l = fresh_lane();
+        la.init(p.A, p.a_bytes, t.m0, p.M, p.lda, t.kb, t.ke, l, wave);
+        lb.init(p.B, p.b_bytes, t.n0, p.N, p.ldb, t.kb, t.ke, l, wave);
+        i32x4 r;
 #pragma unroll
         for (int i = 0; i < DW; ++i) {
-            uint32_t o = la.next(sA);
-            load_blocks<LA>(sA, lds0 + i * SA, la.off, o, wave);
-            o = lb.next(sB);
-            load_blocks<LW>(sB, ldsW + i * SW, lb.off, o, wave);
+            uint32_t o = la.next(r);
+            load_blocks<LA>(r, lds0 + i * SA, la.off, o, wave);
+            o = lb.next(r);
+            load_blocks<LW>(r, ldsW + i * SW, lb.off, o, wave);
         }
-        wait_vm_lgkm0<(DW - 1) * (LA + LW)>();
-        lds_barrier();
-        bf16x8 a0[FM], b0[FN], a1[FM], b1[FN];
+    };
+
+    Tile cur, nxt;
+    if (!tile_of_round(0, nxt)) return;
+    begin(nxt);
+    // (one value for all lanes, here for good: left to the epilogues, its load
+    // has the compiler wait for every load in flight inside the main loop)
+    float peak = 1.0f;
+    if constexpr (EPI != kStats)
+        peak = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, *p.peak)));
+    for (int round = 1;; ++round) {
+        cur = nxt;
+        f32x4 acc[FN][FM];
 #pragma unroll
-        for (int mi = 0; mi < FM; ++mi) a0[mi] = ra.template read<0>(lds0, mi);
+        for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
-        for (int ni = 0; ni < FN; ++ni) b0[ni] = rb.template read<0>(ldsW, ni);
-        constexpr int NM = FM * FN;
-        constexpr int RE = NM - NM / 4;     // substep 0's reads end here, ahead of the barrier's wait
-        constexpr int B1 = NM / 16;         // MFMAs of substep 1 before the barrier
-        // fragments in the order an MFMA substep needs them: b[0], a[..], b[1..]
-        uint32_t aC = lds0, aF = lds0 + DW * SA, wC = ldsW;
-        if constexpr (kAcc) {
-            // Every accumulator in a register of its own from before the loop,
-            // then around it: from the constant zero the compiler rotates them
-            // (364 to 604 moves per stage and spills).
+            for (int mi = 0; mi < FM; ++mi) acc[ni][mi] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        {
+            Reader<AT, BM, FM> ra;
+            Reader<BT, BN, FN> rb;
+            const int l = fresh_lane();
+            ra.init(wm0, l);
+            rb.init(wn0, l);
+            const int KT = (cur.ke - cur.kb + kBK - 1) / kBK;
+            const uint32_t wb = (uint32_t)wave * 1024u;
+            // (stores of the tile before count too, and need not return in order
+            // with these loads: all of both; by the builtin, for the compiler then
+            // knows that nothing of the epilogue is in flight and puts no wait of
+            // its own into the loop)
+            if (kPre && round > 1) __builtin_amdgcn_s_waitcnt(0);
+            else wait_vm_lgkm0<(DW - 1) * (LA + LW)>();
+            lds_barrier();
+            bf16x8 a0[FM], b0[FN], a1[FM], b1[FN];
 #pragma unroll
-            for (int i = 0; i < NM; ++i) asm volatile("" : "+a"(acc[i / FM][slot_row<FM>(i)]));
-        }
-        for (int st = 0; st < KT; ++st) {
-            const uint32_t aN = aC + SA == ldsW ? lds0 : aC + SA, wN = wC + SW == ldsE ? ldsW : wC + SW;
-            if constexpr (kAcc) {   // every accumulator in its own register around the loop
+            for (int mi = 0; mi < FM; ++mi) a0[mi] = ra.template read<0>(lds0, mi);
+#pragma unroll
+            for (int ni = 0; ni < FN; ++ni) b0[ni] = rb.template read<0>(ldsW, ni);
+            constexpr int NM = FM * FN;
+            constexpr int RE = NM - NM / 4;     // substep 0's reads end here, ahead of the barrier's wait
+            constexpr int B1 = NM / 16;         // MFMAs of substep 1 before the barrier
+            i32x4 sA, sB;
+            // fragments in the order an MFMA substep needs them: b[0], a[..], b[1..]
+            uint32_t aC = lds0, aF = lds0 + DW * SA, wC = ldsW;
+            if constexpr (kAcc) {
+                // Every accumulator in a register of its own from before the loop,
+                // then around it: from the constant zero the compiler rotates them
+                // (364 to 604 moves per stage and spills).
 #pragma unroll
                 for (int i = 0; i < NM; ++i) asm volatile("" : "+a"(acc[i / FM][slot_row<FM>(i)]));
             }
-            const uint32_t oA = la.next(sA), oB = lb.next(sB);
-            auto read1 = [&](auto fc) __attribute__((always_inline)) {
-                constexpr int f = decltype(fc)::value;
-                if constexpr (f >= 1 && f <= FM) a1[f - 1] = ra.template read<1>(aC, f - 1);
-                else b1[f == 0 ? 0 : f - FM] = rb.template read<1>(wC, f == 0 ? 0 : f - FM);
-            };
-            auto read0 = [&](auto fc) __attribute__((always_inline)) {
-                constexpr int f = decltype(fc)::value;
-                if constexpr (f >= 1 && f <= FM) a0[f - 1] = ra.template read<0>(aN, f - 1);
-                else b0[f == 0 ? 0 : f - FM] = rb.template read<0>(wN, f == 0 ? 0 : f - FM);
-            };
-            auto loadA = [&](int j) { dma16(sA, la.off[j] + oA, aF + wb + (uint32_t)j * 4096u); };
-            auto loadB = [&](int j) { dma16(sB, lb.off[j] + oB, wC + wb + (uint32_t)j * 4096u); };
-            mfma_run<0, NM, 0, RE, LA, 0, NM, FM, FN>(acc, a0, b0, read1, loadA);
-            mfma_run<0, B1, NM, NM + 1, 0, 0, 1, FM, FN>(acc, a1, b1, read0, loadA);
-            wait_vm_lgkm0<(DW - 1) * LA + (DW - 2) * LW>();
-            lds_barrier();
-            mfma_run<B1, NM, B1, NM, LW, B1, B1 + (NM - B1) * 3 / 4, FM, FN>(acc, a1, b1, read0, loadB);
-            aF = aC;
-            aC = aN;
-            wC = wN;
-        }
-        wait_vm_lgkm0<0>();   // the loads past the end land before the buffers are reused
-        __syncthreads();
-    }
-
-    // thread coordinates the compiler cannot see to be known before the main
-    // loop: what is derived from them is computed here, not kept (spilled)
-    // over the loop
-    int et = lane;
-    asm volatile("" : "+v"(et));
-    // lane (er, eq) holds of block (mi, ni): row er, columns 4 eq + 0..3
-    const int er = et & 15, eq = et >> 4;
-    if constexpr (EPI == kStats) {
-        const int c0 = n0 + wn0 + 4 * eq;
-        const bool edge = n0 + BN > p.N;
-        float2 *out = p.parts + (size_t)(2 * tn + (wave & 1)) * (size_t)p.M;
+            for (int st = 0; st < KT; ++st) {
+                const uint32_t aN = aC + SA == ldsW ? lds0 : aC + SA, wN = wC + SW == ldsE ? ldsW : wC + SW;
+                if constexpr (kAcc) {
 #pragma unroll
-        for (int mi = 0; mi < FM; ++mi) {
-            const int m = m0 + wm0 + mi * 16 + er;
-            float z[FN][4], mx = -INFINITY;
-#pragma unroll
-            for (int ni = 0; ni < FN; ++ni)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[ni][e] = edge && c0 + ni * 16 + e >= p.N ? -INFINITY : acc[ni][mi][e];
-                    mx = fmaxf(mx, z[ni][e]);
+                    for (int i = 0; i < NM; ++i) asm volatile("" : "+a"(acc[i / FM][slot_row<FM>(i)]));
                 }
-            mx = wave16_max(mx);
-            const float sub = mx == -INFINITY ? 0.0f : mx;   // no column of this half is inside
-            float sum = 0.0f;
+                const uint32_t oA = la.next(sA), oB = lb.next(sB);
+                auto read1 = [&](auto fc) __attribute__((always_inline)) {
+                    constexpr int f = decltype(fc)::value;
+                    if constexpr (f >= 1 && f <= FM) a1[f - 1] = ra.template read<1>(aC, f - 1);
+                    else b1[f == 0 ? 0 : f - FM] = rb.template read<1>(wC, f == 0 ? 0 : f - FM);
+                };
+                auto read0 = [&](auto fc) __attribute__((always_inline)) {
+                    constexpr int f = decltype(fc)::value;
+                    if constexpr (f >= 1 && f <= FM) a0[f - 1] = ra.template read<0>(aN, f - 1);
+                    else b0[f == 0 ? 0 : f - FM] = rb.template read<0>(wN, f == 0 ? 0 : f - FM);
+                };
+                auto loadA = [&](int j) { dma16(sA, la.off[j] + oA, aF + wb + (uint32_t)j * 4096u); };
+                auto loadB = [&](int j) { dma16(sB, lb.off[j] + oB, wC + wb + (uint32_t)j * 4096u); };
+                mfma_run<0, NM, 0, RE, LA, 0, NM, FM, FN>(acc, a0, b0, read1, loadA);
+                mfma_run<0, B1, NM, NM + 1, 0, 0, 1, FM, FN>(acc, a1, b1, read0, loadA);
+                wait_vm_lgkm0<(DW - 1) * LA + (DW - 2) * LW>();
+                lds_barrier();
+                mfma_run<B1, NM, B1, NM, LW, B1, B1 + (NM - B1) * 3 / 4, FM, FN>(acc, a1, b1, read0, loadB);
+                aF = aC;
+                aC = aN;
+                wC = wN;
+            }
+            wait_vm_lgkm0<0>();   // the loads past the end land before the buffers are reused
+            __syncthreads();
+        }
+        const bool more = tile_of_round(round, nxt);
+        if (kPre && more) begin(nxt);
+
+        const int et = fresh_lane();
+        // lane (er, eq) holds of block (mi, ni): row er, columns 4 eq + 0..3
+        const int er = et & 15, eq = et >> 4;
+        const int m1 = cur.m0 + wm0, n1 = cur.n0 + wn0;   // of this wave
+        const int c0 = n1 + 4 * eq;
+        const bool edge = cur.n0 + BN > p.N;
+        char *const region = smem + (kPre ? DW * SA : 0) + wave * kRegion;
+        if constexpr (EPI == kStats) {
+            // in units of log 2, so that an exponential is one multiply-add and one
+            // v_exp_f32; the maximum is rounded before it is used
+            float2 *out = p.parts + (size_t)(2 * cur.tn + (wave & 1)) * (size_t)p.M;
 #pragma unroll
-            for (int ni = 0; ni < FN; ++ni)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[ni][e] - sub) * kLog2e);
-            sum = wave16_sum(sum);
-            if (m < p.M) {
-                if (eq == 0) out[m] = make_float2(mx, sum);
-                const int64_t t = p.target[m] - p.v0 - c0;
+            for (int mi = 0; mi < FM; ++mi) {
+                const int m = m1 + mi * 16 + er;
+                float z[FN][4], mx = -INFINITY;
 #pragma unroll
                 for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (t == ni * 16 + e && c0 + ni * 16 + e < p.N) p.tlogit[m] = z[ni][e];
+                    for (int e = 0; e < 4; ++e) z[ni][e] = acc[ni][mi][e];
+                if (edge) {
+#pragma unroll
+                    for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c0 + ni * 16 + e >= p.N) z[ni][e] = -INFINITY;
+                }
+#pragma unroll
+                for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mx = fmaxf(mx, z[ni][e]);
+                mx = row_max(mx) * kLog2e;
+                const float sub = mx == -INFINITY ? 0.0f : mx;   // no column of this half is inside
+                float sum = 0.0f;
+#pragma unroll
+                for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[ni][e], kLog2e, -sub));
+                sum = row_sum(sum);
+                if (m < p.M) {
+                    if (eq == 0) out[m] = make_float2(mx, sum);
+                    const int64_t t = p.target[m] - p.v0 - c0;
+                    if (t >= 0 && t < WN && t + c0 < p.N) {
+#pragma unroll
+                        for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (t == ni * 16 + e) p.tlogit[m] = z[ni][e];
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);   // (rows of blocks started together spill)
             }
-        }
-    } else {
-        // Each wave turns 32 rows at a time to row order through a region of
-        // the freed stage buffers and stores whole rows of its columns, 16
-        // bytes per lane. The regions are the wave's own and its LDS operations
-        // run in order: nothing waits between a write and its read.
-        const float peak = EPI == kDz ? 0.0f : *p.peak;
-        if constexpr (EPI == kPart) {
-            // fp32: 16-byte chunk c of row r at chunk c ^ (r & 7)
+        } else if constexpr (EPI == kPart) {
+            // Each wave turns 32 rows at a time to row order through its region and
+            // stores whole rows of its columns, 32 bytes per lane; 16-byte chunk c
+            // of row r at chunk c ^ (r & 7). The region is the wave's own and its
+            // LDS operations run in order: nothing waits between a write and its
+            // read.
             constexpr int CPR = 2 * FN, NIT = 32 * CPR / 64, RB = FN * 64;
-            static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
-            char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
-            auto to_lds = [&](int mi) {
-                char *w = region[mi & 1] + er * RB;
+#pragma unroll
+            for (int mi = 0; mi < FM / 2; ++mi) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int ni = 0; ni < FN; ++ni)
-                        *reinterpret_cast<f32x4 *>(w + h * 16 * RB + (((4 * ni + eq) ^ (er & 7)) << 4)) =
+                        *reinterpret_cast<f32x4 *>(region + (er + h * 16) * RB + (((4 * ni + eq) ^ (er & 7)) << 4)) =
                             acc[ni][2 * mi + h];
                 asm volatile("" ::: "memory");
-            };
-            to_lds(0);
-#pragma unroll
-            for (int mi = 0; mi < FM / 2; ++mi) {
-                if (mi + 1 < FM / 2) to_lds(mi + 1);
 #pragma unroll
                 for (int it = 0; it < NIT; ++it) {
                     const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
-                    const char *w = region[mi & 1] + row * RB;
+                    const char *w = region + row * RB;
                     // half of the lanes take their two chunks in the other order,
                     // so that 8 lanes read 8 different bank groups
                     const int sw = (j >> 2) & 1;
@@ -407,9 +466,9 @@ void tile_kernel(const TileParams p) {
                         x0[e] = peak * (sw ? u1[e] : u0[e]);
                         x1[e] = peak * (sw ? u0[e] : u1[e]);
                     }
-                    const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
+                    const int m = m1 + mi * 32 + row, n = n1 + j * 8;
                     if (m < p.M && n < p.N) {   // N is a multiple of 8
-                        const size_t at = ((size_t)slice * (size_t)p.M + (size_t)m) * (size_t)p.N + n;
+                        const size_t at = ((size_t)cur.slice * (size_t)p.M + (size_t)m) * (size_t)p.N + n;
                         if (p.part_in) {
                             x0 += *reinterpret_cast<const f32x4 *>(p.part_in + at);
                             x1 += *reinterpret_cast<const f32x4 *>(p.part_in + at + 4);
@@ -424,68 +483,90 @@ void tile_kernel(const TileParams p) {
                         }
                     }
                 }
+                asm volatile("" ::: "memory");
             }
         } else {
-            // rounded in the accumulators' layout, so that half the bytes go
-            // through LDS: chunk c of row r at chunk c ^ (r & SW)
-            constexpr int CPR = 2 * FN, RB = FN * 32, SW_ = CPR % 8 == 0 ? 7 : 3;
-            static_assert(4 * 32 * RB <= NA * SA && 4 * 32 * RB <= DW * SW, "a region fits its buffers");
-            char *const region[2] = {smem + wave * 32 * RB, smem + NA * SA + wave * 32 * RB};
-            // dz: the rows' statistics, all loaded at once
+            // The same, rounded to bf16 in the accumulators' layout, so that half
+            // the bytes go through LDS: chunk c of row r at chunk c ^ (r & SWZ).
+            constexpr int CPR = 2 * FN, RB = FN * 32, SWZ = CPR % 8 == 0 ? 7 : 3;
+            // dz: the rows' weights and statistics, all loaded at once
             float lse[EPI == kDz ? FM : 1], g[EPI == kDz ? FM : 1];
             int t[EPI == kDz ? FM : 1];   // the target's place from this lane's first column, or -1
             if constexpr (EPI == kDz) {
-                const float top = *p.peak;
 #pragma unroll
                 for (int mi = 0; mi < FM; ++mi) {
-                    const int m = min(m0 + wm0 + mi * 16 + er, p.M - 1);
-                    const int64_t id = p.target[m], at = id - p.v0 - (n0 + wn0 + 4 * eq);
-                    lse[mi] = p.lse[m];
-                    g[mi] = id < 0 ? 0.0f : p.grad[m] / top;
+                    const int m = min(m1 + mi * 16 + er, p.M - 1);
+                    const int64_t id = p.target[m], at = id - p.v0 - c0;
+                    lse[mi] = p.lse[m] * kLog2e;
+                    g[mi] = id < 0 ? 0.0f : p.grad[m] / peak;
                     t[mi] = id < 0 || at < 0 || at >= WN ? -1 : (int)at;
                 }
             }
-            const int c0 = n0 + wn0 + 4 * eq;
-            const bool edge = n0 + BN > p.N;
-            auto to_lds = [&](int mi2) {
-                char *w = region[mi2 & 1] + er * RB;
+            uint16_t *out = EPI == kDz ? p.dz : p.C;
+            const int ld = EPI == kDz ? p.ldz : p.N;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int mi2 = 0; mi2 < FM / 2; ++mi2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int mi = 2 * mi2 + h;
+                    char *w = region + (er + h * 16) * RB + 8 * (eq & 1);
+                    f32x4 x[FN];
 #pragma unroll
                     for (int ni = 0; ni < FN; ++ni) {
-                        f32x4 x = acc[ni][2 * mi2 + h];
+                        x[ni] = acc[ni][mi];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if constexpr (EPI == kDz) {
-                                const int mi = 2 * mi2 + h;
-                                const float pr = __builtin_amdgcn_exp2f((x[e] - lse[mi]) * kLog2e);
-                                x[e] = g[mi] * (pr - (t[mi] == ni * 16 + e ? 1.0f : 0.0f));
-                                // (a row without weight is zero whatever its logits are)
-                                if (g[mi] == 0.0f || (edge && c0 + ni * 16 + e >= p.N)) x[e] = 0.0f;
+                                const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[ni][e], kLog2e, -lse[mi]));
+                                x[ni][e] = g[mi] == 0.0f ? 0.0f : g[mi] * pr;   // (0 whatever the logits are)
                             } else {
-                                x[e] *= peak;
+                                x[ni][e] *= peak;
                             }
                         }
-                        *reinterpret_cast<u32x2 *>(w + h * 16 * RB + (((2 * ni + (eq >> 1)) ^ (er & SW_)) << 4) +
-                                                   8 * (eq & 1)) =
-                            u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
                     }
-                asm volatile("" ::: "memory");
-            };
-            uint16_t *out = EPI == kDz ? p.dz : p.C;
-            const int ld = EPI == kDz ? p.ldz : p.N;
-            to_lds(0);
+                    if constexpr (EPI == kDz) {
+                        if (__ballot(t[mi] >= 0)) {   // (a few per cent of the blocks hold a target)
 #pragma unroll
-            for (int mi = 0; mi < FM / 2; ++mi) {
-                if (mi + 1 < FM / 2) to_lds(mi + 1);
+                            for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (t[mi] == ni * 16 + e) x[ni][e] -= g[mi];
+                        }
+                        if (edge) {
+#pragma unroll
+                            for (int ni = 0; ni < FN; ++ni)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e)
+                                    if (c0 + ni * 16 + e >= p.N) x[ni][e] = 0.0f;
+                        }
+                    }
+#pragma unroll
+                    for (int ni = 0; ni < FN; ++ni)
+                        *reinterpret_cast<u32x2 *>(w + (((2 * ni + (eq >> 1)) ^ (er & SWZ)) << 4)) =
+                            u32x2{pack_bf16x2(x[ni][0], x[ni][1]), pack_bf16x2(x[ni][2], x[ni][3])};
+                    __builtin_amdgcn_sched_barrier(0);   // (rows of blocks started together spill)
+                }
+                asm volatile("" ::: "memory");
 #pragma unroll
                 for (int it = 0; it < FN; ++it) {
                     const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
-                    const u32x4 o = *reinterpret_cast<const u32x4 *>(region[mi & 1] + row * RB + ((j ^ (row & SW_)) << 4));
-                    const int m = m0 + wm0 + mi * 32 + row, n = n0 + wn0 + j * 8;
-                    if (m < p.M && n < ld) *reinterpret_cast<u32x4 *>(out + (size_t)m * (size_t)ld + n) = o;
+                    const u32x4 o = *reinterpret_cast<const u32x4 *>(region + row * RB + ((j ^ (row & SWZ)) << 4));
+                    const int m = m1 + mi2 * 32 + row, n = n1 + j * 8;
+                    u32x4 *to = reinterpret_cast<u32x4 *>(out + (size_t)m * (size_t)ld + n);
+                    if (m < p.M && n < ld) {
+                        // dW is not read again here: its stores pass through the caches
+                        if constexpr (AT) __builtin_nontemporal_store(o, to);
+                        else *to = o;
+                    }
                 }
+                asm volatile("" ::: "memory");
             }
+        }
+        if (!more) return;
+        if (!kPre) {
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            begin(nxt);
         }
     }
 }
@@ -513,7 +594,7 @@ __global__ __launch_bounds__(1024) void peak_kernel(int M, const int64_t *target
     *peak = x > 0.0f && x < INFINITY ? x : 1.0f;
 }
 
-// Joins a row's parts: lse = max + log sum_i s_i exp(m_i - max). ROWS rows per
+// Joins a row's parts: lse = log 2 (max + log2 sum_i s_i 2^(m_i - max)). ROWS rows per
 // workgroup, 256 / ROWS threads each: 16 rows read whole 128-byte lines of the
 // parts; few rows (at most 256) take a workgroup each (8 rows of 1000 parts:
 // 20.6 us with 16).
@@ -528,7 +609,7 @@ __global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, con
     float mx = -INFINITY, sum = 0.0f;
     auto add = [&](float2 x) {
         const float top = fmaxf(mx, x.x), sub = top == -INFINITY ? 0.0f : top;
-        sum = sum * __builtin_amdgcn_exp2f((mx - sub) * kLog2e) + x.y * __builtin_amdgcn_exp2f((x.x - sub) * kLog2e);
+        sum = sum * __builtin_amdgcn_exp2f(mx - sub) + x.y * __builtin_amdgcn_exp2f(x.x - sub);
         mx = top;
     };
     if (m < M) {
@@ -545,7 +626,7 @@ __global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, con
         }
     }
     if (q != 0 || m >= M) return;
-    const float l = mx + logf(sum);
+    const float l = (mx + log2f(sum)) * kLn2;
     const int64_t t = target[m];
     float tl = 0.0f;
     if (t >= v0 && t - v0 < V) tl = tlogit[m];
@@ -579,6 +660,7 @@ __global__ __launch_bounds__(256) void join_slices_kernel(size_t count4, int sli
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= count4) return;
     f32x4 x = part[i];
+#pragma unroll 8
     for (int s = 1; s < slices; ++s) x += part[(size_t)s * count4 + i];
     *reinterpret_cast<u32x2 *>(out + 4 * i) = u32x2{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])};
 }
@@ -591,18 +673,21 @@ hipError_t launch_tiles(TileParams p, const TilePlan &pl, hipStream_t stream) {
     p.tiles_n = pl.tiles_n;
     p.slices = pl.slices;
     p.kslice = pl.kslice;
-    p.group_m = kTileShapes[pl.cfg].rows == 256 ? 4 : 8;
-    const dim3 grid((unsigned)(pl.tiles_m * pl.tiles_n * pl.slices));
+    p.group_m = kTiles[pl.cfg].rows == 256 ? 4 : 8;
+    const int64_t items = (int64_t)pl.tiles_m * pl.tiles_n * pl.slices;
+    const dim3 grid((unsigned)std::min<int64_t>(items, kCUs * kTiles[pl.cfg].wg_per_cu));
+    // (a template instance for each row of kTiles)
     switch (pl.cfg) {
-    case kTile256: tile_kernel<256, 256, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile256x192: tile_kernel<256, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile256x128: tile_kernel<256, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile192: tile_kernel<192, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile128x192: tile_kernel<128, 192, 3, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile128: tile_kernel<128, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile128Deep: tile_kernel<128, 128, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    case kTile128x64Deep: tile_kernel<128, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
-    default: tile_kernel<64, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 0: tile_kernel<256, 256, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 1: tile_kernel<256, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 2: tile_kernel<256, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 3: tile_kernel<192, 192, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 4: tile_kernel<128, 192, 3, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 5: tile_kernel<128, 128, 2, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 6: tile_kernel<128, 128, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 7: tile_kernel<128, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    case 8: tile_kernel<64, 64, 4, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
+    default: tile_kernel<64, 256, 3, AT, BT, EPI><<<grid, kThreads, 0, stream>>>(p); break;
     }
     return hipGetLastError();
 }
@@ -648,7 +733,7 @@ int op_xent_workspace(int M, int V, int K, int backward, int piece, size_t *byte
         const BackwardPlan b = plan_backward(M, V, K, piece);
         *bytes = b.dz_bytes + b.part_bytes;
     } else {
-        *bytes = forward_bytes(plan_pair(M, V, K, false), M);
+        *bytes = forward_bytes(plan_pair(kLogits, K % 64 != 0, M, V, K, false), M);
     }
     return COMPASS_OK;
 }
@@ -662,7 +747,7 @@ int op_xent_forward(int M, int V, int K, const void *H, const void *W, const int
     if (misaligned(H) || misaligned(W) || misaligned(ws))
         return set_error(COMPASS_ERR_INVALID, "H, W and the workspace must be 16-byte aligned");
     if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
-    const PairPlan pl = plan_pair(M, V, K, false);
+    const PairPlan pl = plan_pair(kLogits, K % 64 != 0, M, V, K, false);
     if (ws_bytes < forward_bytes(pl, M))
         return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, forward_bytes(pl, M));
     int cus;
@@ -727,6 +812,7 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
     peak_kernel<<<1, 1024, 0, s>>>(M, target, grad, peak);
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return hip_error(e, "peak launch");
     const uint64_t h_bytes = (uint64_t)M * (uint64_t)K * 2;
+    const bool ragged = K % 64 != 0;
     for (int i = 0; i < b.pieces.count; ++i) {
         const int c0 = i * b.pieces.cols, cols = std::min(b.pieces.cols, V - c0);
         const uint16_t *Wp = (const uint16_t *)W + (size_t)c0 * (size_t)K;
@@ -746,7 +832,7 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         p.peak = peak;
         p.dz = dz;
         p.ldz = dz_columns(cols);
-        hipError_t e = launch_pair<false, false, kDz>(p, plan_pair(M, p.ldz, K, false), false, s);
+        hipError_t e = launch_pair<false, false, kDz>(p, plan_pair(kGradLogits, ragged, M, p.ldz, K, false), false, s);
         if (e != hipSuccess) return hip_error(e, "dz launch");
 
         TileParams q{};
@@ -761,7 +847,7 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         q.R = M;
         q.peak = peak;
         q.C = (uint16_t *)dW + (size_t)c0 * (size_t)K;
-        e = launch_pair<true, true, kStore>(q, plan_pair(cols, K, M, true), true, s);
+        e = launch_pair<true, true, kStore>(q, plan_pair(kGradWeight, ragged, cols, K, M, true), true, s);
         if (e != hipSuccess) return hip_error(e, "dW launch");
         // dH += dz W over this piece
         q.B = Wp;
