@@ -383,30 +383,45 @@ def compass_gemm_noalloc(A, W, C, P=None, stream=None) -> None:
 
 
 # ------------------------------------------- the ends of a model (see the header)
+class _Kinds:
+    """The dtypes of operands: bf16 values as bf16 or as raw patterns, elements
+    of operators of either type, fp32, indices."""
+
+    def __init__(self):
+        import torch
+        self.bits = (torch.bfloat16, torch.int16)
+        self.elements = (torch.bfloat16, torch.float32)
+        self.float = (torch.float32,)
+        self.index = (torch.int64,)
+
+
+_kinds = None
+
+
+def _find_kinds() -> _Kinds:
+    global _kinds
+    if _kinds is None:
+        _kinds = _Kinds()
+    return _kinds
+
+
 def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False) -> None:
     """Raise ValueError unless x is a GPU tensor of the given shape whose dtype
-    is one of `kinds` (names), contiguous or, with `rows`, in rows of
-    consecutive elements that do not overlap. Plain int addresses are the
-    caller's responsibility."""
+    is one of `kinds`, contiguous or, with `rows`, in rows of consecutive
+    elements that do not overlap. Plain int addresses are the caller's
+    responsibility."""
     if x is None or isinstance(x, int):
+        return
+    if x.shape == shape and x.dtype in kinds and x.is_cuda and x.is_contiguous():
         return
     if x.shape != shape:
         raise ValueError(f"{what}: shape {_shape_of(x)}, expected {tuple(shape)}")
-    kind = str(x.dtype)[6:]
-    if kind not in kinds:
-        raise ValueError(f"{what}: {kind}, expected {' or '.join(kinds)}")
+    if x.dtype not in kinds:
+        raise ValueError(f"{what}: {x.dtype}, expected {' or '.join(str(k) for k in kinds)}")
     if not x.is_cuda:
         raise ValueError(f"{what}: must be on the GPU")
-    if x.is_contiguous():
-        return
     if not rows or (shape[1] > 1 and x.stride(1) != 1) or (shape[0] > 1 and x.stride(0) < shape[1]):
         raise ValueError(f"{what}: must be contiguous" + (" within rows" if rows else ""))
-
-
-_BITS = ("bfloat16", "int16")        # bf16 values, as bf16 or as raw patterns
-_ELEMENTS = ("bfloat16", "float32")  # operators of either type
-_FLOAT = ("float32",)
-_INDEX = ("int64",)
 
 
 def _kind(x) -> int:
@@ -420,7 +435,7 @@ def _ld(x) -> int:
 def _ws(x) -> int:
     if x is None or not x.is_cuda or not x.is_contiguous():
         raise ValueError("workspace: must be a contiguous GPU tensor")
-    return x.numel() * x.element_size()
+    return x.nbytes
 
 
 def compass_xent_workspace(M: int, V: int, K: int, backward: bool = False, piece: int = 0) -> int:
@@ -434,14 +449,15 @@ def compass_xent_workspace(M: int, V: int, K: int, backward: bool = False, piece
 def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0, stream=None) -> None:
     """lse, tlogit and loss (M each, fp32; loss may be None) of hidden states H
     (M x K) and the vocabulary rows W (V x K) from id v0; see the header."""
+    kinds = _kinds or _find_kinds()
     M, K = H.shape
     V = W.shape[0]
-    _typed(H, "H", (M, K), _BITS)
-    _typed(W, "W", (V, K), _BITS)
-    _typed(target, "target", (M,), _INDEX)
-    _typed(lse, "lse", (M,), _FLOAT)
-    _typed(tlogit, "tlogit", (M,), _FLOAT)
-    _typed(loss, "loss", (M,), _FLOAT)
+    _typed(H, "H", (M, K), kinds.bits)
+    _typed(W, "W", (V, K), kinds.bits)
+    _typed(target, "target", (M,), kinds.index)
+    _typed(lse, "lse", (M,), kinds.float)
+    _typed(tlogit, "tlogit", (M,), kinds.float)
+    _typed(loss, "loss", (M,), kinds.float)
     rc = (_lib or lib()).compass_xent_forward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(tlogit),
                                               _addr(loss), _addr(workspace), _ws(workspace), _stream(stream))
     if rc < 0:
@@ -450,12 +466,13 @@ def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0
 
 def compass_xent_join(lse_parts, tlogit_parts, target, lse, loss, stream=None) -> None:
     """lse and loss of the whole vocabulary from the n ranks' shards (n x M)."""
+    kinds = _kinds or _find_kinds()
     n, M = lse_parts.shape
-    _typed(lse_parts, "lse_parts", (n, M), _FLOAT)
-    _typed(tlogit_parts, "tlogit_parts", (n, M), _FLOAT)
-    _typed(target, "target", (M,), _INDEX)
-    _typed(lse, "lse", (M,), _FLOAT)
-    _typed(loss, "loss", (M,), _FLOAT)
+    _typed(lse_parts, "lse_parts", (n, M), kinds.float)
+    _typed(tlogit_parts, "tlogit_parts", (n, M), kinds.float)
+    _typed(target, "target", (M,), kinds.index)
+    _typed(lse, "lse", (M,), kinds.float)
+    _typed(loss, "loss", (M,), kinds.float)
     _check(lib().compass_xent_join(n, M, _addr(lse_parts), _addr(tlogit_parts), _addr(target), _addr(lse), _addr(loss),
                                    _stream(stream)), "compass_xent_join")
 
@@ -463,15 +480,16 @@ def compass_xent_join(lse_parts, tlogit_parts, target, lse, loss, stream=None) -
 def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 0, piece: int = 0,
                           stream=None) -> None:
     """Gradients dH (M x K) and dW (V x K) of sum(grad * loss); see the header."""
+    kinds = _kinds or _find_kinds()
     M, K = H.shape
     V = W.shape[0]
-    _typed(H, "H", (M, K), _BITS)
-    _typed(W, "W", (V, K), _BITS)
-    _typed(target, "target", (M,), _INDEX)
-    _typed(lse, "lse", (M,), _FLOAT)
-    _typed(grad, "grad", (M,), _FLOAT)
-    _typed(dH, "dH", (M, K), _BITS)
-    _typed(dW, "dW", (V, K), _BITS)
+    _typed(H, "H", (M, K), kinds.bits)
+    _typed(W, "W", (V, K), kinds.bits)
+    _typed(target, "target", (M,), kinds.index)
+    _typed(lse, "lse", (M,), kinds.float)
+    _typed(grad, "grad", (M,), kinds.float)
+    _typed(dH, "dH", (M, K), kinds.bits)
+    _typed(dW, "dW", (V, K), kinds.bits)
     rc = (_lib or lib()).compass_xent_backward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(grad),
                                                _addr(dH), _addr(dW), piece, _addr(workspace), _ws(workspace),
                                                _stream(stream))
@@ -481,8 +499,9 @@ def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 
 
 def _params(gamma, beta, N: int) -> int:
     """Checks the norm's parameters (either may be None) and gives their type."""
-    _typed(gamma, "gamma", (N,), _ELEMENTS)
-    _typed(beta, "beta", (N,), _ELEMENTS)
+    kinds = _kinds or _find_kinds()
+    _typed(gamma, "gamma", (N,), kinds.elements)
+    _typed(beta, "beta", (N,), kinds.elements)
     if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
         raise ValueError(f"gamma and beta: {gamma.dtype} and {beta.dtype}, expected one type")
     one = gamma if gamma is not None else beta
@@ -492,12 +511,13 @@ def _params(gamma, beta, N: int) -> int:
 def compass_norm_forward(x, gamma, beta, y, mean, rstd, eps: float = 1e-5, stream=None) -> None:
     """Layer norm y (M x N, of x's type) with its statistics mean and rstd (M,
     fp32); gamma and beta may be None. Rows of x and y may lie apart."""
+    kinds = _kinds or _find_kinds()
     M, N = x.shape
-    _typed(x, "x", (M, N), _ELEMENTS, rows=True)
-    _typed(y, "y", (M, N), (str(x.dtype)[6:],), rows=True)
+    _typed(x, "x", (M, N), kinds.elements, rows=True)
+    _typed(y, "y", (M, N), (x.dtype,), rows=True)
     ptype = _params(gamma, beta, N)
-    _typed(mean, "mean", (M,), _FLOAT)
-    _typed(rstd, "rstd", (M,), _FLOAT)
+    _typed(mean, "mean", (M,), kinds.float)
+    _typed(rstd, "rstd", (M,), kinds.float)
     rc = (_lib or lib()).compass_norm_forward(M, N, _kind(x), ptype, _addr(x), _ld(x), _addr(gamma), _addr(beta), eps,
                                               _addr(y), _ld(y), _addr(mean), _addr(rstd), _stream(stream))
     if rc < 0:
@@ -514,16 +534,17 @@ def compass_norm_workspace(M: int, N: int) -> int:
 def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None) -> None:
     """dx (of x's type), dgamma and dbeta (N, fp32; None: not wanted) of
     compass_norm_forward; gamma may be None."""
+    kinds = _kinds or _find_kinds()
     M, N = x.shape
-    kind = (str(x.dtype)[6:],)
-    _typed(x, "x", (M, N), _ELEMENTS, rows=True)
+    kind = (x.dtype,)
+    _typed(x, "x", (M, N), kinds.elements, rows=True)
     _typed(dy, "dy", (M, N), kind, rows=True)
     _typed(dx, "dx", (M, N), kind, rows=True)
     ptype = _params(gamma, None, N)
-    _typed(mean, "mean", (M,), _FLOAT)
-    _typed(rstd, "rstd", (M,), _FLOAT)
-    _typed(dgamma, "dgamma", (N,), _FLOAT)
-    _typed(dbeta, "dbeta", (N,), _FLOAT)
+    _typed(mean, "mean", (M,), kinds.float)
+    _typed(rstd, "rstd", (M,), kinds.float)
+    _typed(dgamma, "dgamma", (N,), kinds.float)
+    _typed(dbeta, "dbeta", (N,), kinds.float)
     rc = (_lib or lib()).compass_norm_backward(M, N, _kind(x), ptype, _addr(dy), _ld(dy), _addr(x), _ld(x), _addr(gamma),
                                                _addr(mean), _addr(rstd), _addr(dx), _ld(dx), _addr(dgamma),
                                                _addr(dbeta), _addr(workspace),
@@ -535,11 +556,12 @@ def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace
 def compass_embed_forward(ids, table, y, scale: float = 1.0, v0: int = 0, stream=None) -> None:
     """y[t] = scale * table[ids[t] - v0] (T x K, of the table's type), zeros for
     ids outside the table's rows."""
+    kinds = _kinds or _find_kinds()
     V, K = table.shape
     T = ids.shape[0]
-    _typed(ids, "ids", (T,), _INDEX)
-    _typed(table, "table", (V, K), _ELEMENTS, rows=True)
-    _typed(y, "y", (T, K), (str(table.dtype)[6:],), rows=True)
+    _typed(ids, "ids", (T,), kinds.index)
+    _typed(table, "table", (V, K), kinds.elements, rows=True)
+    _typed(y, "y", (T, K), (table.dtype,), rows=True)
     rc = (_lib or lib()).compass_embed_forward(T, V, K, _kind(table), _addr(ids), v0, _addr(table), _ld(table), scale,
                                                _addr(y), _ld(y), _stream(stream))
     if rc < 0:
@@ -557,11 +579,12 @@ def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: i
                            stream=None) -> None:
     """dtable (V x K) of compass_embed_forward from dy (T x K); with accumulate,
     added to what dtable holds."""
+    kinds = _kinds or _find_kinds()
     T, K = dy.shape
     V = dtable.shape[0]
-    _typed(ids, "ids", (T,), _INDEX)
-    _typed(dy, "dy", (T, K), _ELEMENTS, rows=True)
-    _typed(dtable, "dtable", (V, K), _ELEMENTS, rows=True)
+    _typed(ids, "ids", (T,), kinds.index)
+    _typed(dy, "dy", (T, K), kinds.elements, rows=True)
+    _typed(dtable, "dtable", (V, K), kinds.elements, rows=True)
     rc = (_lib or lib()).compass_embed_backward(T, V, K, _kind(dy), _kind(dtable), _addr(ids), v0, _addr(dy), _ld(dy),
                                                 scale, _addr(dtable), _ld(dtable), 1 if accumulate else 0,
                                                 _addr(workspace), _ws(workspace), _stream(stream))

@@ -363,7 +363,9 @@ bool rows_aligned(const void *p, int64_t ld, int type) {
     return ((uintptr_t)p & 15) == 0 && (size_t)ld * size_of(type) % 16 == 0;
 }
 
-// The smallest group (8 to 256 threads) that holds a row.
+// The smallest group (8 to 256 threads) that holds a row, else 256. (Smaller
+// groups that leave fewer threads past a row's end measured slower: 50257 x 1031
+// bf16, 4000 tokens: 61 us, in 9 blocks of 16 threads 92.)
 Cover cover(int K, int V) {
     const int vectors = (K + V - 1) / V;
     Cover c{3};

@@ -258,8 +258,10 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(int N, int parts, con
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int c = (int)blockIdx.x * 64 + lane;
     float sum = 0.0f;
-    if (c < 2 * N)
+    if (c < 2 * N) {
+#pragma unroll 8
         for (int i = w; i < parts; i += 16) sum += part[(size_t)i * 2 * (size_t)N + c];
+    }
     s[w][lane] = sum;
     __syncthreads();
     if (w != 0 || c >= 2 * N) return;
