@@ -1,5 +1,5 @@
 // How the products of the vocabulary cross entropy are cut: output tiles,
-// slices of the reduction, pieces of the vocabulary. Host only.
+// slices of the reduction, pieces of the vocabulary, and who takes which tile.
 #pragma once
 #include <stddef.h>
 
@@ -77,6 +77,15 @@ inline TilePlan plan_tiles(Product what, bool ragged, int M, int N, int R, int m
         }
     }
     return best;
+}
+
+// Work position of workgroup b of `grid` in its round j, of `total` positions,
+// or -1. Each XCD (workgroups go round-robin over them) walks a run of its own,
+// an eighth of the positions (so all have workgroups, or grid = total).
+__host__ __device__ inline int round_position(int total, int grid, int b, int j) {
+    const int v = b & 7, at = j * ((grid >> 3) + (v < (grid & 7) ? 1 : 0)) + (b >> 3);
+    if (at >= (total >> 3) + (v < (total & 7) ? 1 : 0)) return -1;
+    return v * (total >> 3) + (v < (total & 7) ? v : (total & 7)) + at;
 }
 
 // A product in one launch, or in two along its long axis (rows of C with

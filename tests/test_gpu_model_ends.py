@@ -89,6 +89,61 @@ def test_xent_forward(M, V, K):
     _within("loss", loss, r_loss, z + tol + 2 * U24 * np.abs(r_loss))
 
 
+# sizes that, with those above, take every tile in every product (held to that
+# by tests/test_model_ends_host.py); checked on the GPU in 64 bits
+XENT_TILES = [(6369, 4438, 928), (1747, 4510, 4088), (6370, 939, 2568), (68, 16092, 880), (2, 33544, 136),
+              (135, 32870, 16), (199, 2, 5744), (2, 59446, 80), (2, 4566, 5656), (202, 130, 8200), (257, 31800, 152),
+              (4107, 4588, 72), (1100, 130, 16384), (6039, 5947, 136), (130, 23917, 1680), (8402, 649, 1008),
+              (1242, 33844, 232), (1159, 1976, 6440), (4228, 48807, 72), (300, 4099, 12288), (4489, 1309, 3528),
+              (409, 57510, 952), (387, 17604, 6392)]
+
+
+def _within_gpu(name, got, ref, tol):
+    torch = _torch()
+    assert torch.isfinite(got).all(), name
+    over = (got.double() - ref).abs() - tol
+    assert not (over > 0).any(), f"{name}: {int((over > 0).sum())} of {got.numel()} out of bound, by up to {float(over.max()):.3g}"
+
+
+@pytest.mark.parametrize("M,V,K", XENT_TILES)
+def test_xent_every_tile(M, V, K):
+    print(f"xent tiles {M} {V} {K}", flush=True)
+    torch = _torch()
+    H, W, t = _xent_inputs(M, V, K, 41)
+    h, w = H.double(), W.double()
+    z = h @ w.T
+    kept = t >= 0
+    at = t.clamp(min=0)[:, None]
+    r_lse = torch.logsumexp(z, 1)
+    r_tl = torch.where(kept, z.gather(1, at)[:, 0], 0.0)
+    mag = (h.abs() @ w.abs().T).amax(1)
+    z_tol = 2 * K * U24 * mag
+    tol = z_tol + 2 * U24 * (V + 64 + 4 * mag)
+    lse, tl, loss = _nan(M), _nan(M), _nan(M)
+    C.compass_xent_forward(H, W, t, lse, tl, loss, _scratch(C.compass_xent_workspace(M, V, K)))
+    _within_gpu("lse", lse, r_lse, tol)
+    _within_gpu("tlogit", tl, r_tl, z_tol + 2 * U24 * r_tl.abs())
+    r_loss = torch.where(kept, r_lse - r_tl, 0.0)
+    _within_gpu("loss", loss, r_loss, z_tol + tol + 2 * U24 * r_loss.abs())
+
+    lse = r_lse.float()
+    grad = (_gen(42)(M) * 0.3 + 1.0) / M
+    dH, dW = _backward(H, W, t, lse, grad)
+    g = grad.double()[:, None]
+    p = (z - lse.double()[:, None]).exp_()
+    del z
+    delta = (z_tol + tol + 128 * U24)[:, None] * 1.01
+    err = (1 + U8) * g.abs() * (p * delta + 4 * U24)     # as _dz_error's
+    p.scatter_add_(1, at, -kept.double()[:, None])
+    dz = torch.where(kept[:, None], g, 0.0) * p
+    err += dz.abs() * (U8 + 4 * U24 * (1 + U8))
+    del p
+    for name, got, ref, e, n in (("dH", dH, dz @ w, err @ w.abs() + 2 * V * U24 * (dz.abs() @ w.abs()), V),
+                                 ("dW", dW, dz.T.contiguous() @ h,
+                                  err.T.contiguous() @ h.abs() + 2 * M * U24 * (dz.T.abs().contiguous() @ h.abs()), M)):
+        _within_gpu(name, got, ref, e + U8 * (ref.abs() + e))
+
+
 def _dz_error(H, W, t, lse, grad, v0):
     """Bound on the error of each dz element: the exponent's, the subtraction's
     and the bf16 rounding's."""
