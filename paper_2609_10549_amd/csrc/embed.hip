@@ -25,6 +25,19 @@ namespace {
 
 constexpr int kRun = 32;
 
+// Elements by which a loose fp32 row's vectors are moved back so that they lie
+// on whole 128-byte lines of what is written: a wave's streaming stores then
+// leave no line half written (a masked write costs the memory a read) but at the
+// row's ends. 14785 tokens, 65225 x 3890 fp32: gradient 257 -> 211 us, lookup 61
+// -> 56; bf16 rows, whose end vectors are 8 stores, lose by it (8000 tokens,
+// 20000 x 5001: 92 -> 103). kLineElements: at most so many more elements to cover.
+template <bool LOOSE, class T>
+__device__ __forceinline__ int line_shift(const T *row) {
+    return LOOSE && sizeof(T) == 4 ? (int)(((uintptr_t)row & 127) / sizeof(T)) : 0;
+}
+template <bool LOOSE, class T>
+constexpr int kLineElements = LOOSE && sizeof(T) == 4 ? 31 : 0;
+
 // How a kernel's workgroups of 256 threads cover rows of K elements: groups of
 // 2^shift threads, a vector of V elements each; blockIdx.y counts the column
 // blocks of rows that one group does not cover.
@@ -45,15 +58,17 @@ template <class T, int V, bool LOOSE, int TOKENS>
 __global__ __launch_bounds__(256) void lookup_kernel(Cover cov, int tokens, int K, int64_t v0, int vocab,
                                                      const int64_t *__restrict__ ids, const T *__restrict__ table,
                                                      int64_t ldt, float scale, T *y, int64_t ldy) {
-    const int t0 = cov.group((int)blockIdx.x) * TOKENS, c = cov.column<V>();
-    if (t0 >= tokens || c >= K) return;
+    const int t0 = cov.group((int)blockIdx.x) * TOKENS;
+    if (t0 >= tokens) return;
     Pack<T, V> p[TOKENS];
     bool inside[TOKENS];
+    int c[TOKENS];
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
         const int64_t row = t0 + j < tokens ? ids[t0 + j] - v0 : -1;
         inside[j] = row >= 0 && row < vocab;
-        if (inside[j]) p[j] = load_pack<T, V, LOOSE>(table + row * ldt, c, K);
+        c[j] = cov.column<V>() - line_shift<LOOSE>(y + (int64_t)(t0 + j) * ldy);
+        if (inside[j]) p[j] = load_pack<T, V, LOOSE>(table + row * ldt, c[j], K);
     }
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
@@ -62,7 +77,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(Cover cov, int tokens, int 
         unpack(p[j], f);
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] = inside[j] ? f[e] * scale : 0.0f;
-        store_pack<T, V, LOOSE>(y + (int64_t)(t0 + j) * ldy, c, K, f);
+        if (c[j] < K) store_pack<T, V, LOOSE>(y + (int64_t)(t0 + j) * ldy, c[j], K, f);
     }
 }
 
@@ -201,6 +216,12 @@ struct Gradient {
     int64_t ldt;
 };
 
+// Column of this thread's vector, `col` on lines, in a table row.
+template <class G, bool LOOSE>
+__device__ __forceinline__ int row_column(const Gradient &g, int row, int col) {
+    return col - line_shift<LOOSE>((const G *)g.dtable + (int64_t)row * g.ldt);
+}
+
 // A table row's sums from column c on, scaled, to the table or onto it.
 template <class G, int V, bool LOOSE, bool ACC>
 __device__ __forceinline__ void put_row(const Gradient &g, int row, int c, float (&f)[V]) {
@@ -234,7 +255,7 @@ template <class T, class G, int V, bool LOOSE, bool ACC>
 __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
     const int per = 256 >> g.cov.shift;
     const int block_wgs = (g.blocks + per - 1) / per, token_wgs = ((g.T + kAhead - 1) / kAhead + per - 1) / per;
-    const int readers = block_wgs + token_wgs, at = (int)blockIdx.x, c = g.cov.column<V>();
+    const int readers = block_wgs + token_wgs, at = (int)blockIdx.x, col = g.cov.column<V>();
     const T *dy = (const T *)g.dy;
     float f[V] = {};
     if (at < block_wgs) {
@@ -242,9 +263,9 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
         if (b >= g.blocks) return;
         const int row = g.sorted[b * kRun];
         if (row == g.V || g.sorted[b * kRun + kRun - 1] != row) return;
-        add_rows<T, V, LOOSE>(f, g.cov.shift, c, g.K, g.order, dy, g.ld, b * kRun, b * kRun + kRun);
+        add_rows<T, V, LOOSE>(f, g.cov.shift, col, g.K, g.order, dy, g.ld, b * kRun, b * kRun + kRun);
         // (read back soon: no streaming)
-        store_pack<float, V, false, false>(g.part + (size_t)b * (size_t)g.ldp, c, g.ldp, f);
+        store_pack<float, V, false, false>(g.part + (size_t)b * (size_t)g.ldp, col, g.ldp, f);
     } else if (at < readers) {
         const int i0 = g.cov.group(at - block_wgs) * kAhead;
         if (i0 >= g.T) return;
@@ -259,7 +280,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
             const int tok = __shfl(my_tok, j, kAhead);
             // not a run of the groups before, nor an id outside the table
             if (j < n && row[j] != before && row[j] != g.V)
-                p[j] = load_pack<T, V, LOOSE, ACC>(dy + (int64_t)tok * g.ld, c, g.K);
+                p[j] = load_pack<T, V, LOOSE, ACC>(dy + (int64_t)tok * g.ld, row_column<G, LOOSE>(g, row[j], col), g.K);
         }
         int lo = i0;   // of the run at j
 #pragma unroll
@@ -271,6 +292,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
             if (begins) lo = i0 + j;
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] = begins ? d[e] : f[e] + d[e];
+            const int c = row_column<G, LOOSE>(g, row[j], col);
             if (j + 1 < n) {
                 if (row[j + 1] == row[j]) continue;
             } else {   // the run may go on
@@ -288,7 +310,8 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
 #pragma unroll
         for (int i = 0; i < kZeroRows; ++i)
             if (row0 + i < g.V && start[i] == start[i + 1])
-                store_pack<G, V, LOOSE>((G *)g.dtable + (int64_t)(row0 + i) * g.ldt, c, g.K, f);
+                store_pack<G, V, LOOSE>((G *)g.dtable + (int64_t)(row0 + i) * g.ldt,
+                                        row_column<G, LOOSE>(g, row0 + i, col), g.K, f);
     }
 }
 
@@ -306,7 +329,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
     const int row = g.sorted[b * kRun];
     if (row == g.V || g.sorted[b * kRun + kRun - 1] != row || (b > 0 && g.sorted[(b - 1) * kRun] == row)) return;
     const int lane = (int)threadIdx.x & 63, w = (int)threadIdx.x >> 6;
-    const int c = ((int)blockIdx.y * 64 + lane) * V;
+    const int c = row_column<G, LOOSE>(g, row, ((int)blockIdx.y * 64 + lane) * V);
     const int lo = g.first[row], hi = g.first[row + 1], b1 = hi / kRun;
     float f[V] = {};
     auto add = [&](const float (&d)[V]) {
@@ -323,7 +346,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
 #pragma unroll 4
     for (int i = b + w; i < b1; i += 16) {
         float d[V];
-        unpack(load_pack<float, V, false>(g.part + (size_t)i * (size_t)g.ldp, c, g.ldp), d);
+        unpack(load_pack<float, V, LOOSE>(g.part + (size_t)i * (size_t)g.ldp, c, LOOSE ? g.K : g.ldp), d);
         add(d);
     }
 #pragma unroll 2
@@ -403,9 +426,10 @@ Scratch scratch_of(int T, int V, int K) {
 template <class T, int V, bool LOOSE>
 void lookup(int tokens, int K, int vocab, const int64_t *ids, int64_t v0, const void *table, int64_t ldt, float scale,
             void *y, int64_t ldy, hipStream_t s) {
-    const Cover c = cover(K, V);
+    const int cols = K + kLineElements<LOOSE, T>;
+    const Cover c = cover(cols, V);
     const auto go = [&](auto kernel, int per) {
-        kernel<<<grid(c, wgs_of(c, (tokens + per - 1) / per), K, V), 256, 0, s>>>(
+        kernel<<<grid(c, wgs_of(c, (tokens + per - 1) / per), cols, V), 256, 0, s>>>(
             c, tokens, K, v0, vocab, ids, (const T *)table, ldt, scale, (T *)y, ldy);
     };
     if (tokens < 4096) go(lookup_kernel<T, V, LOOSE, 1>, 1);
@@ -414,11 +438,12 @@ void lookup(int tokens, int K, int vocab, const int64_t *ids, int64_t v0, const 
 
 template <class D, class G, int V, bool LOOSE, bool ACC>
 void launch_gradient(Gradient g, hipStream_t s) {
-    g.cov = cover(g.K, V);
+    const int cols = g.K + kLineElements<LOOSE, G>;
+    g.cov = cover(cols, V);
     const int64_t zeros = ACC ? 0 : ((int64_t)g.V + kZeroRows - 1) / kZeroRows;
     const int64_t wgs = wgs_of(g.cov, g.blocks) + wgs_of(g.cov, (g.T + kAhead - 1) / kAhead) + wgs_of(g.cov, zeros);
-    rows_kernel<D, G, V, LOOSE, ACC><<<grid(g.cov, wgs, g.K, V), 256, 0, s>>>(g);
-    const dim3 by_block((unsigned)g.blocks, (unsigned)((g.K + 64 * V - 1) / (64 * V)));
+    rows_kernel<D, G, V, LOOSE, ACC><<<grid(g.cov, wgs, cols, V), 256, 0, s>>>(g);
+    const dim3 by_block((unsigned)g.blocks, (unsigned)((cols + 64 * V - 1) / (64 * V)));
     if (g.blocks > 0) long_rows_kernel<D, G, V, LOOSE, ACC><<<by_block, 1024, 0, s>>>(g);
 }
 template <class D, class G, int V>

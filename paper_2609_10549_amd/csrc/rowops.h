@@ -55,10 +55,10 @@ __device__ __forceinline__ Pack<T, V> pack(const float (&f)[V]) {
 __device__ __forceinline__ void put_element(Bf16 *p, float x) { p->bits = (uint16_t)bf16_bits(x); }
 __device__ __forceinline__ void put_element(float *p, float x) { *p = x; }
 
-// Elements [i, i + V) of a row of N. LOOSE: a row starts on any element and its
-// last vector may be cut by its end (the card loads and stores 16 bytes from
-// any address, at the cost of the extra line they touch); otherwise rows start
-// on 16 bytes and hold whole vectors. STREAM: passes through the caches without
+// Elements [i, i + V) of a row of N. LOOSE: a row starts on any element and a
+// vector may be cut by either end (the card loads and stores 16 bytes from any
+// address, at the cost of the extra line they touch); otherwise rows start on
+// 16 bytes and hold whole vectors. STREAM: passes through the caches without
 // staying. An output of more than the caches hold would otherwise be allocated
 // line by line and written back later: what a kernel measured with and without
 // stands there.
@@ -71,7 +71,7 @@ template <class T, int V, bool LOOSE, bool STREAM = false>
 __device__ __forceinline__ Pack<T, V> load_pack(const T *row, int i, int N) {
     typedef typename Piece<LOOSE>::type At;
     Pack<T, V> p;
-    if (i + V <= N) {
+    if ((!LOOSE || i >= 0) && i + V <= N) {
         const At *from = reinterpret_cast<const At *>(row + i);
 #pragma unroll
         for (int j = 0; j < Pack<T, V>::Q; ++j) p.q[j] = STREAM ? __builtin_nontemporal_load(from + j) : from[j];
@@ -80,10 +80,10 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T *row, int i, int N) {
 #pragma unroll
     for (int j = 0; j < Pack<T, V>::Q; ++j) p.q[j] = u32x4_{0, 0, 0, 0};
     if constexpr (LOOSE) {
-        if (i < N) {
+        if (i < N && i > -V) {
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                if (i + e < N) {
+                if (i + e >= 0 && i + e < N) {
                     if constexpr (sizeof(T) == 4) p.q[e / 4][e % 4] = __builtin_bit_cast(uint32_t, row[i + e]);
                     else p.q[0][e / 2] |= (uint32_t)row[i + e].bits << (16 * (e & 1));
                 }
@@ -94,7 +94,7 @@ __device__ __forceinline__ Pack<T, V> load_pack(const T *row, int i, int N) {
 template <class T, int V, bool LOOSE, bool STREAM = true>
 __device__ __forceinline__ void store_pack(T *row, int i, int N, const float (&f)[V]) {
     typedef typename Piece<LOOSE>::type At;
-    if (i + V <= N) {
+    if ((!LOOSE || i >= 0) && i + V <= N) {
         const Pack<T, V> p = pack<T, V>(f);
         At *to = reinterpret_cast<At *>(row + i);
 #pragma unroll
@@ -103,10 +103,10 @@ __device__ __forceinline__ void store_pack(T *row, int i, int N, const float (&f
             else to[j] = p.q[j];
         }
     } else if constexpr (LOOSE) {
-        if (i < N) {
+        if (i < N && i > -V) {
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                if (i + e < N) put_element(row + i + e, f[e]);
+                if (i + e >= 0 && i + e < N) put_element(row + i + e, f[e]);
         }
     }
 }
