@@ -7,7 +7,7 @@
 // runs in token order whatever the machine does), every table row finds its
 // run in the sorted order, and one pass writes the table, each element once:
 // the sum of the run's rows, or zero. A long run (a frequent token) would be
-// one workgroup's long walk, so blocks of kRun sorted positions that lie inside
+// one workgroup's long walk, so blocks of sorted positions that lie inside
 // one run are summed beside that pass, all at once, and a second, short one
 // adds those sums for the rows that have any. No atomics anywhere.
 #include <hip/hip_runtime.h>
@@ -23,7 +23,12 @@ namespace compass {
 
 namespace {
 
-constexpr int kRun = 32;
+// Sorted positions of a block: 2^run_shift(T). Short batches take small blocks,
+// so that the runs without one (below twice a block) are short walks too; in
+// long ones the blocks' own workgroups count (500 tokens, 6283 x 1031 fp32: 16
+// positions 22 us, 32 27; 8000 tokens, 20000 x 5001 bf16: 86 and 94; 32768 tokens,
+// 50257 x 4096: 158 and 146).
+constexpr int run_shift(int T) { return T < 16384 ? 4 : 5; }
 
 // Elements by which a loose fp32 row's vectors are moved back so that they lie
 // on whole 128-byte lines of what is written: a wave's streaming stores then
@@ -205,7 +210,7 @@ __device__ __forceinline__ void add_rows(float (&f)[V], int shift, int c, int K,
 struct Gradient {
     Cover cov;
     int T, K, V;
-    int blocks;                     // kRun sorted positions each
+    int blocks, shift;              // 2^shift sorted positions each
     const int *order, *sorted, *first;
     float *part;                    // [blocks][ldp]
     int ldp;
@@ -238,7 +243,7 @@ __device__ __forceinline__ void put_row(const Gradient &g, int row, int c, float
 }
 
 // One launch of three kinds of groups, each kind rounded up to a workgroup:
-//   blocks: the sum of a block of kRun sorted positions that lies inside one run;
+//   blocks: the sum of a block of sorted positions that lies inside one run;
 //   tokens: kAhead sorted positions; writes the table rows of the runs that
 //     begin there, but for one that holds such a block;
 //   zeros (not with ACC): kZeroRows table rows, those without tokens.
@@ -261,9 +266,10 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
     if (at < block_wgs) {
         const int b = g.cov.group(at);
         if (b >= g.blocks) return;
-        const int row = g.sorted[b * kRun];
-        if (row == g.V || g.sorted[b * kRun + kRun - 1] != row) return;
-        add_rows<T, V, LOOSE>(f, g.cov.shift, col, g.K, g.order, dy, g.ld, b * kRun, b * kRun + kRun);
+        const int from = b << g.shift, to = from + (1 << g.shift);
+        const int row = g.sorted[from];
+        if (row == g.V || g.sorted[to - 1] != row) return;
+        add_rows<T, V, LOOSE>(f, g.cov.shift, col, g.K, g.order, dy, g.ld, from, to);
         // (read back soon: no streaming)
         store_pack<float, V, false, false>(g.part + (size_t)b * (size_t)g.ldp, col, g.ldp, f);
     } else if (at < readers) {
@@ -297,7 +303,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const Gradient g) {
                 if (row[j + 1] == row[j]) continue;
             } else {   // the run may go on
                 const int hi = g.first[row[j] + 1];
-                if ((lo + kRun - 1) / kRun < hi / kRun) continue;
+                if (((lo + (1 << g.shift) - 1) >> g.shift) < (hi >> g.shift)) continue;
                 add_rows<T, V, LOOSE>(f, g.cov.shift, c, g.K, g.order, dy, g.ld, i0 + n, hi);
             }
             put_row<G, V, LOOSE, ACC>(g, row[j], c, f);
@@ -326,11 +332,11 @@ template <class T, class G, int V, bool LOOSE, bool ACC>
 __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
     __shared__ float s[16][64 * V];
     const int b = (int)blockIdx.x;
-    const int row = g.sorted[b * kRun];
-    if (row == g.V || g.sorted[b * kRun + kRun - 1] != row || (b > 0 && g.sorted[(b - 1) * kRun] == row)) return;
+    const int row = g.sorted[b << g.shift];
+    if (row == g.V || g.sorted[((b + 1) << g.shift) - 1] != row || (b > 0 && g.sorted[(b - 1) << g.shift] == row)) return;
     const int lane = (int)threadIdx.x & 63, w = (int)threadIdx.x >> 6;
     const int c = row_column<G, LOOSE>(g, row, ((int)blockIdx.y * 64 + lane) * V);
-    const int lo = g.first[row], hi = g.first[row + 1], b1 = hi / kRun;
+    const int lo = g.first[row], hi = g.first[row + 1], b1 = hi >> g.shift;
     float f[V] = {};
     auto add = [&](const float (&d)[V]) {
 #pragma unroll
@@ -342,7 +348,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
         add(d);
     };
 #pragma unroll 2
-    for (int i = lo + w; i < b * kRun; i += 16) token(i);
+    for (int i = lo + w; i < b << g.shift; i += 16) token(i);
 #pragma unroll 4
     for (int i = b + w; i < b1; i += 16) {
         float d[V];
@@ -350,7 +356,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
         add(d);
     }
 #pragma unroll 2
-    for (int i = b1 * kRun + w; i < hi; i += 16) token(i);
+    for (int i = (b1 << g.shift) + w; i < hi; i += 16) token(i);
 #pragma unroll
     for (int e = 0; e < V; ++e) s[w][e * 64 + lane] = f[e];
     __syncthreads();
@@ -419,7 +425,7 @@ Scratch scratch_of(int T, int V, int K) {
     s.chunk_sorted = s.chunk_order + (T > kChunk ? list : 0);
     s.part = s.chunk_sorted + (T > kChunk ? list : 0);
     s.ldp = (K + 7) / 8 * 8;
-    s.bytes = s.part + (size_t)(T / kRun) * (size_t)s.ldp * 4;
+    s.bytes = s.part + (size_t)(T >> run_shift(T)) * (size_t)s.ldp * 4;
     return s;
 }
 
@@ -514,8 +520,8 @@ int op_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *
         merge_kernel<<<by64, 1024, 0, s>>>(T, chunk_order, chunk_sorted, order, sorted);
     }
     runs_kernel<<<dim3((unsigned)(V / 256 + 1)), 256, 0, s>>>(T, V, sorted, first);
-    const Gradient g{{}, T, K, V, T / kRun, order, sorted, first, (float *)(w + sc.part), sc.ldp, dy, ldy, scale, dtable,
-                     ldt};
+    const Gradient g{{}, T, K, V, T >> run_shift(T), run_shift(T), order, sorted, first, (float *)(w + sc.part),
+                     sc.ldp, dy, ldy, scale, dtable, ldt};
     const bool d32 = dtype == COMPASS_F32, g32 = gtype == COMPASS_F32;
     // one vector width for both sides: 16 bytes of the smaller type
     const bool loose = K % (d32 && g32 ? 4 : 8) != 0 || !rows_aligned(dy, ldy, dtype) || !rows_aligned(dtable, ldt, gtype);
