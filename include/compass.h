@@ -343,8 +343,10 @@ int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void
  *   library's choice, at most 512 MiB of dz); sums over pieces stay in fp32.
  *
  * H, W, dH, dW and the workspace are 16-byte aligned and packed; none may
- * overlap another. Limits: K a multiple of 8 up to 2^17, M up to 2^20, V up to
- * 2^24. */
+ * overlap another. H is read for every row: a NaN in a row without a target
+ * leaves that row's dH zero, but reaches dW. Limits: K a multiple of 8 up to
+ * 2^17, M up to 2^20, V up to 2^24, min(M, 256) rows of a caller's `piece`
+ * within 1 GiB of dz. */
 int compass_xent_workspace(int M, int V, int K, int backward, int piece, size_t *bytes);
 int compass_xent_forward(int M, int V, int K, const void *H, const void *W, const int64_t *target, int64_t v0,
                          float *lse, float *tlogit, float *loss, void *workspace, size_t workspace_bytes,
@@ -355,7 +357,7 @@ int compass_xent_backward(int M, int V, int K, const void *H, const void *W, con
                           const float *lse, const float *grad, void *dH, void *dW, int piece, void *workspace,
                           size_t workspace_bytes, void *stream);
 
-/* Layer norm over rows of N elements (at most 16384):
+/* Layer norm over M rows (at most 2^21) of N elements (at most 16384):
  *   mean = sum x / N, rstd = 1 / sqrt(sum (x - mean)^2 / N + eps),
  *   y = (x - mean) rstd gamma + beta
  * x, y, dy, dx: M rows of type dtype, ld elements apart (>= N). gamma, beta: N

@@ -275,6 +275,7 @@ __global__ __launch_bounds__(1024) void norm_params_kernel(int N, int parts, con
 }
 
 constexpr int kMaxCols = 16384;   // a row's elements in 1024 threads' registers, 16 each
+constexpr int kMaxRows = 1 << 21; // 1024 threads each, below the 2^32 of a launch
 
 int hip_error(hipError_t e, const char *what) {
     return set_error(COMPASS_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
@@ -356,7 +357,8 @@ int check(int M, int N, int dtype, int ptype) {
     if (M < 1 || N < 1) return set_error(COMPASS_ERR_INVALID, "need positive M and N");
     if ((dtype != COMPASS_BF16 && dtype != COMPASS_F32) || (ptype != COMPASS_BF16 && ptype != COMPASS_F32))
         return set_error(COMPASS_ERR_INVALID, "unknown element type %d or %d", dtype, ptype);
-    if (N > kMaxCols) return set_error(COMPASS_ERR_UNSUPPORTED, "rows of %d elements, at most %d", N, kMaxCols);
+    if (N > kMaxCols || M > kMaxRows)
+        return set_error(COMPASS_ERR_UNSUPPORTED, "%d rows of %d elements, at most %d of %d", M, N, kMaxRows, kMaxCols);
     return COMPASS_OK;
 }
 

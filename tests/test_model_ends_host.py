@@ -124,6 +124,11 @@ def test_xent_refusals_before_enqueue():
     out = ctypes.c_size_t()
     assert lib.compass_xent_workspace(4, 8, 8, 1, -1, ctypes.byref(out)) == C.ERR_INVALID
     assert lib.compass_xent_workspace(4, 8, 8, 0, 0, None) == C.ERR_INVALID
+    # 256 rows of a piece over 1 GiB of dz (as the library's own choice is not)
+    assert lib.compass_xent_workspace(256, 1 << 24, 8, 1, (1 << 21) + 64, ctypes.byref(out)) == C.ERR_UNSUPPORTED
+    assert bwd(M=256, V=1 << 24, piece=(1 << 21) + 64, n=1 << 40) == C.ERR_UNSUPPORTED
+    for M in (1, 16, 255, 256, 4096, 1 << 20):
+        assert lib.compass_xent_workspace(M, 1 << 24, 8, 1, 0, ctypes.byref(out)) == C.OK
     with pytest.raises(C.CompassError):
         C.compass_xent_workspace(4, 8, 9)
 
@@ -138,6 +143,7 @@ def test_norm_refusals_before_enqueue():
         for kw in (dict(M=0), dict(N=0), dict(d=2), dict(p=-1), dict(x=None), dict(mean=None), dict(rstd=None),
                    dict(ldx=7), dict(x=Q), dict(g=Q)):
             assert call(**kw) == C.ERR_INVALID, kw
+        assert call(M=(1 << 21) + 1) == C.ERR_UNSUPPORTED
         assert call(N=16385, **({"ldx": 16385, "ldy": 16385} if call is fwd else {"ldx": 16385})) == C.ERR_UNSUPPORTED
     for kw in (dict(y=None), dict(ldy=7), dict(eps=-1.0), dict(eps=float("nan")), dict(y=Q), dict(b=Q)):
         assert fwd(**kw) == C.ERR_INVALID, kw
