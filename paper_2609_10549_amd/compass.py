@@ -405,23 +405,26 @@ def _find_kinds() -> _Kinds:
     return _kinds
 
 
-def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False) -> None:
-    """Raise ValueError unless x is a GPU tensor of the given shape whose dtype
-    is one of `kinds`, contiguous or, with `rows`, in rows of consecutive
-    elements that do not overlap. Plain int addresses are the caller's
-    responsibility."""
+def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False):
+    """The address of x, a GPU tensor of the given shape whose dtype is one of
+    `kinds`, contiguous or, with `rows`, in rows of consecutive elements that do
+    not overlap; ValueError for any other. None and plain int addresses pass as
+    they are, the latter on the caller's responsibility. (One call per operand
+    for the check and the address: a single-token operator takes as long on the
+    host as on the GPU.)"""
     if x is None or isinstance(x, int):
-        return
-    if x.shape == shape and x.dtype in kinds and x.is_cuda and x.is_contiguous():
-        return
+        return x
+    if x.shape == shape and x.dtype in kinds and x.is_cuda and (
+            x.is_contiguous() or rows and (shape[1] <= 1 or x.stride(1) == 1)
+            and (shape[0] <= 1 or x.stride(0) >= shape[1])):
+        return x.data_ptr()
     if x.shape != shape:
         raise ValueError(f"{what}: shape {_shape_of(x)}, expected {tuple(shape)}")
     if x.dtype not in kinds:
         raise ValueError(f"{what}: {x.dtype}, expected {' or '.join(str(k) for k in kinds)}")
     if not x.is_cuda:
         raise ValueError(f"{what}: must be on the GPU")
-    if not rows or (shape[1] > 1 and x.stride(1) != 1) or (shape[0] > 1 and x.stride(0) < shape[1]):
-        raise ValueError(f"{what}: must be contiguous" + (" within rows" if rows else ""))
+    raise ValueError(f"{what}: must be contiguous" + (" within rows" if rows else ""))
 
 
 def _kind(x) -> int:
@@ -432,10 +435,11 @@ def _ld(x) -> int:
     return x.stride(0) if x.shape[0] > 1 else x.shape[1]
 
 
-def _ws(x) -> int:
+def _ws(x) -> tuple:
+    """Address and bytes of a workspace."""
     if x is None or not x.is_cuda or not x.is_contiguous():
         raise ValueError("workspace: must be a contiguous GPU tensor")
-    return x.nbytes
+    return x.data_ptr(), x.nbytes
 
 
 def compass_xent_workspace(M: int, V: int, K: int, backward: bool = False, piece: int = 0) -> int:
@@ -449,77 +453,63 @@ def compass_xent_workspace(M: int, V: int, K: int, backward: bool = False, piece
 def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0, stream=None) -> None:
     """lse, tlogit and loss (M each, fp32; loss may be None) of hidden states H
     (M x K) and the vocabulary rows W (V x K) from id v0; see the header."""
-    kinds = _kinds or _find_kinds()
+    k = _kinds or _find_kinds()
     M, K = H.shape
     V = W.shape[0]
-    _typed(H, "H", (M, K), kinds.bits)
-    _typed(W, "W", (V, K), kinds.bits)
-    _typed(target, "target", (M,), kinds.index)
-    _typed(lse, "lse", (M,), kinds.float)
-    _typed(tlogit, "tlogit", (M,), kinds.float)
-    _typed(loss, "loss", (M,), kinds.float)
-    rc = (_lib or lib()).compass_xent_forward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(tlogit),
-                                              _addr(loss), _addr(workspace), _ws(workspace), _stream(stream))
+    rc = (_lib or lib()).compass_xent_forward(
+        M, V, K, _typed(H, "H", (M, K), k.bits), _typed(W, "W", (V, K), k.bits), _typed(target, "target", (M,), k.index),
+        v0, _typed(lse, "lse", (M,), k.float), _typed(tlogit, "tlogit", (M,), k.float),
+        _typed(loss, "loss", (M,), k.float), *_ws(workspace), _stream(stream))
     if rc < 0:
         _check(rc, "compass_xent_forward")
 
 
 def compass_xent_join(lse_parts, tlogit_parts, target, lse, loss, stream=None) -> None:
     """lse and loss of the whole vocabulary from the n ranks' shards (n x M)."""
-    kinds = _kinds or _find_kinds()
+    k = _kinds or _find_kinds()
     n, M = lse_parts.shape
-    _typed(lse_parts, "lse_parts", (n, M), kinds.float)
-    _typed(tlogit_parts, "tlogit_parts", (n, M), kinds.float)
-    _typed(target, "target", (M,), kinds.index)
-    _typed(lse, "lse", (M,), kinds.float)
-    _typed(loss, "loss", (M,), kinds.float)
-    _check(lib().compass_xent_join(n, M, _addr(lse_parts), _addr(tlogit_parts), _addr(target), _addr(lse), _addr(loss),
-                                   _stream(stream)), "compass_xent_join")
+    rc = (_lib or lib()).compass_xent_join(
+        n, M, _typed(lse_parts, "lse_parts", (n, M), k.float), _typed(tlogit_parts, "tlogit_parts", (n, M), k.float),
+        _typed(target, "target", (M,), k.index), _typed(lse, "lse", (M,), k.float), _typed(loss, "loss", (M,), k.float),
+        _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_xent_join")
 
 
 def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 0, piece: int = 0,
                           stream=None) -> None:
     """Gradients dH (M x K) and dW (V x K) of sum(grad * loss); see the header."""
-    kinds = _kinds or _find_kinds()
+    k = _kinds or _find_kinds()
     M, K = H.shape
     V = W.shape[0]
-    _typed(H, "H", (M, K), kinds.bits)
-    _typed(W, "W", (V, K), kinds.bits)
-    _typed(target, "target", (M,), kinds.index)
-    _typed(lse, "lse", (M,), kinds.float)
-    _typed(grad, "grad", (M,), kinds.float)
-    _typed(dH, "dH", (M, K), kinds.bits)
-    _typed(dW, "dW", (V, K), kinds.bits)
-    rc = (_lib or lib()).compass_xent_backward(M, V, K, _addr(H), _addr(W), _addr(target), v0, _addr(lse), _addr(grad),
-                                               _addr(dH), _addr(dW), piece, _addr(workspace), _ws(workspace),
-                                               _stream(stream))
+    rc = (_lib or lib()).compass_xent_backward(
+        M, V, K, _typed(H, "H", (M, K), k.bits), _typed(W, "W", (V, K), k.bits), _typed(target, "target", (M,), k.index),
+        v0, _typed(lse, "lse", (M,), k.float), _typed(grad, "grad", (M,), k.float), _typed(dH, "dH", (M, K), k.bits),
+        _typed(dW, "dW", (V, K), k.bits), piece, *_ws(workspace), _stream(stream))
     if rc < 0:
         _check(rc, "compass_xent_backward")
 
 
-def _params(gamma, beta, N: int) -> int:
-    """Checks the norm's parameters (either may be None) and gives their type."""
-    kinds = _kinds or _find_kinds()
-    _typed(gamma, "gamma", (N,), kinds.elements)
-    _typed(beta, "beta", (N,), kinds.elements)
-    if gamma is not None and beta is not None and gamma.dtype != beta.dtype:
+def _params(gamma, beta, N: int, kinds: tuple) -> tuple:
+    """The addresses and the type of the norm's parameters (either may be None)."""
+    g, b = _typed(gamma, "gamma", (N,), kinds), _typed(beta, "beta", (N,), kinds)
+    if gamma is None:
+        return g, b, F32 if beta is None else _kind(beta)
+    if beta is not None and gamma.dtype != beta.dtype:
         raise ValueError(f"gamma and beta: {gamma.dtype} and {beta.dtype}, expected one type")
-    one = gamma if gamma is not None else beta
-    return F32 if one is None else _kind(one)
+    return g, b, _kind(gamma)
 
 
 def compass_norm_forward(x, gamma, beta, y, mean, rstd, eps: float = 1e-5, stream=None) -> None:
     """Layer norm y (M x N, of x's type) with its statistics mean and rstd (M,
     fp32); gamma and beta may be None. Rows of x and y may lie apart."""
-    kinds = _kinds or _find_kinds()
-    M, N = x.shape
-    _typed(x, "x", (M, N), kinds.elements, rows=True)
-    _typed(y, "y", (M, N), (x.dtype,), rows=True)
-    ptype = _params(gamma, beta, N)
-    _typed(mean, "mean", (M,), kinds.float)
-    _typed(rstd, "rstd", (M,), kinds.float)
-    rc = (_lib or lib()).compass_norm_forward(M, N, _kind(x), ptype, _addr(x), _ld(x), _addr(gamma), _addr(beta), eps,
-                                              _addr(y), _ld(y), _addr(mean), _addr(rstd), _stream(stream))
+    k = _kinds or _find_kinds()
+    shape = M, N = x.shape
+    g, b, ptype = _params(gamma, beta, N, k.elements)
+    rc = (_lib or lib()).compass_norm_forward(
+        M, N, _kind(x), ptype, _typed(x, "x", shape, k.elements, True), _ld(x), g, b, eps,
+        _typed(y, "y", shape, (x.dtype,), True), _ld(y), _typed(mean, "mean", (M,), k.float),
+        _typed(rstd, "rstd", (M,), k.float), _stream(stream))
     if rc < 0:
         _check(rc, "compass_norm_forward")
 
@@ -534,21 +524,15 @@ def compass_norm_workspace(M: int, N: int) -> int:
 def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None) -> None:
     """dx (of x's type), dgamma and dbeta (N, fp32; None: not wanted) of
     compass_norm_forward; gamma may be None."""
-    kinds = _kinds or _find_kinds()
-    M, N = x.shape
+    k = _kinds or _find_kinds()
+    shape = M, N = x.shape
     kind = (x.dtype,)
-    _typed(x, "x", (M, N), kinds.elements, rows=True)
-    _typed(dy, "dy", (M, N), kind, rows=True)
-    _typed(dx, "dx", (M, N), kind, rows=True)
-    ptype = _params(gamma, None, N)
-    _typed(mean, "mean", (M,), kinds.float)
-    _typed(rstd, "rstd", (M,), kinds.float)
-    _typed(dgamma, "dgamma", (N,), kinds.float)
-    _typed(dbeta, "dbeta", (N,), kinds.float)
-    rc = (_lib or lib()).compass_norm_backward(M, N, _kind(x), ptype, _addr(dy), _ld(dy), _addr(x), _ld(x), _addr(gamma),
-                                               _addr(mean), _addr(rstd), _addr(dx), _ld(dx), _addr(dgamma),
-                                               _addr(dbeta), _addr(workspace),
-                                               0 if workspace is None else _ws(workspace), _stream(stream))
+    g, _, ptype = _params(gamma, None, N, k.elements)
+    rc = (_lib or lib()).compass_norm_backward(
+        M, N, _kind(x), ptype, _typed(dy, "dy", shape, kind, True), _ld(dy), _typed(x, "x", shape, k.elements, True),
+        _ld(x), g, _typed(mean, "mean", (M,), k.float), _typed(rstd, "rstd", (M,), k.float),
+        _typed(dx, "dx", shape, kind, True), _ld(dx), _typed(dgamma, "dgamma", (N,), k.float),
+        _typed(dbeta, "dbeta", (N,), k.float), *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
     if rc < 0:
         _check(rc, "compass_norm_backward")
 
@@ -556,14 +540,12 @@ def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace
 def compass_embed_forward(ids, table, y, scale: float = 1.0, v0: int = 0, stream=None) -> None:
     """y[t] = scale * table[ids[t] - v0] (T x K, of the table's type), zeros for
     ids outside the table's rows."""
-    kinds = _kinds or _find_kinds()
-    V, K = table.shape
+    k = _kinds or _find_kinds()
+    shape = V, K = table.shape
     T = ids.shape[0]
-    _typed(ids, "ids", (T,), kinds.index)
-    _typed(table, "table", (V, K), kinds.elements, rows=True)
-    _typed(y, "y", (T, K), (table.dtype,), rows=True)
-    rc = (_lib or lib()).compass_embed_forward(T, V, K, _kind(table), _addr(ids), v0, _addr(table), _ld(table), scale,
-                                               _addr(y), _ld(y), _stream(stream))
+    rc = (_lib or lib()).compass_embed_forward(
+        T, V, K, _kind(table), _typed(ids, "ids", (T,), k.index), v0, _typed(table, "table", shape, k.elements, True),
+        _ld(table), scale, _typed(y, "y", (T, K), (table.dtype,), True), _ld(y), _stream(stream))
     if rc < 0:
         _check(rc, "compass_embed_forward")
 
@@ -579,15 +561,13 @@ def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: i
                            stream=None) -> None:
     """dtable (V x K) of compass_embed_forward from dy (T x K); with accumulate,
     added to what dtable holds."""
-    kinds = _kinds or _find_kinds()
+    k = _kinds or _find_kinds()
     T, K = dy.shape
     V = dtable.shape[0]
-    _typed(ids, "ids", (T,), kinds.index)
-    _typed(dy, "dy", (T, K), kinds.elements, rows=True)
-    _typed(dtable, "dtable", (V, K), kinds.elements, rows=True)
-    rc = (_lib or lib()).compass_embed_backward(T, V, K, _kind(dy), _kind(dtable), _addr(ids), v0, _addr(dy), _ld(dy),
-                                                scale, _addr(dtable), _ld(dtable), 1 if accumulate else 0,
-                                                _addr(workspace), _ws(workspace), _stream(stream))
+    rc = (_lib or lib()).compass_embed_backward(
+        T, V, K, _kind(dy), _kind(dtable), _typed(ids, "ids", (T,), k.index), v0,
+        _typed(dy, "dy", (T, K), k.elements, True), _ld(dy), scale, _typed(dtable, "dtable", (V, K), k.elements, True),
+        _ld(dtable), 1 if accumulate else 0, *_ws(workspace), _stream(stream))
     if rc < 0:
         _check(rc, "compass_embed_backward")
 
