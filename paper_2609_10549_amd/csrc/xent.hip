@@ -42,6 +42,7 @@ enum Epilogue : int {
     kDz = 1,      // dz in bf16
     kStore = 2,   // the product in bf16
     kPart = 3,    // fp32 partial sums of the product
+    kStream = 4,  // kStore by stores that pass through the caches
 };
 
 struct TileParams {
@@ -62,7 +63,7 @@ struct TileParams {
     const float *lse, *grad;
     uint16_t *dz;                // grad / *peak (exp(z - lse) - [target])
     int ldz;                     // columns [N, ldz) are zero
-    const float *peak;           // kStore, kPart: the product is scaled by it
+    float *peak;                 // kStore, kPart: the product is scaled by it
     // kStore, and kPart's last sum
     uint16_t *C;                 // bf16, rows of N
     // kPart
@@ -226,6 +227,25 @@ __device__ __forceinline__ float row_sum(float x) {
     return a + b;
 }
 
+// The largest |grad| of a row with a target (1 without any). dz is stored as
+// its multiple, and the products are scaled back in fp32: with one weight for
+// all rows, as in a mean, the multiple is exactly 1, and -1 at the targets'
+// columns is exact where grad itself would round by the same 2^-9 or so in
+// every row (8192 x 50257 x 4096, mean loss: dH and dW off by 2.6e-3 of their norm,
+// with it 1.9e-3; 1.7e-3 is their own rounding to bf16).
+__device__ __forceinline__ float peak_of(float largest) {
+    return largest > 0.0f && largest < INFINITY ? largest : 1.0f;
+}
+__device__ __forceinline__ float wave_max(float x) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    return x;
+}
+// Up to so many rows dz's own workgroups find it (and leave it to the products),
+// more take a launch (backward, found here: 1 x 2000 x 1024 21.6 -> 20.2 us,
+// 250 x 20000 x 1024 63.3 -> 63.5).
+constexpr int kOwnPeakRows = 256;
+
 // BM x BN tiles, 4 waves, 2 x 2 over the tile. The main loop (stages of 64,
 // DW + 1 buffers of A and DW of B, counted waits, one barrier per stage, LDS
 // reads and loads one at a time between the MFMAs) is gemm_kernel's; see there
@@ -239,7 +259,7 @@ __device__ __forceinline__ float row_sum(float x) {
 // tile's edges cost beside its stages: 8192 x 50257 x 1024 forward 985 us with a
 // workgroup per tile, 915 with the next tile's loads under the epilogue and
 // exponentials of one multiply-add each. Few rows: W from memory, 8 x 32000 x
-// 4096 38 us (6.8 TB/s).
+// 4096 44 to 51 us (5.2 to 6.0 TB/s; 38 on the same W again).
 template <int BM, int BN, int DW, bool AT, bool BT, int EPI>
 __global__ __launch_bounds__(kThreads, (160 << 10) / (((DW + 1) * BM + DW * BN) * 128))
 void tile_kernel(const TileParams p) {
@@ -313,8 +333,19 @@ void tile_kernel(const TileParams p) {
     // (one value for all lanes, here for good: left to the epilogues, its load
     // has the compiler wait for every load in flight inside the main loop)
     float peak = 1.0f;
+    if constexpr (EPI == kDz) {
+        if (p.M <= kOwnPeakRows) {   // every wave for itself
+            float x = 0.0f;
+#pragma unroll
+            for (int m = lane; m < kOwnPeakRows; m += 64)
+                if (m < p.M) x = fmaxf(x, p.target[m] >= 0 ? fabsf(p.grad[m]) : 0.0f);
+            peak = peak_of(wave_max(x));
+            if (blockIdx.x == 0 && tid == 0) *p.peak = peak;
+        }
+    }
+    if (EPI != kStats && !(EPI == kDz && p.M <= kOwnPeakRows)) peak = *p.peak;
     if constexpr (EPI != kStats)
-        peak = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, *p.peak)));
+        peak = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, peak)));
     for (int round = 1;; ++round) {
         cur = nxt;
         f32x4 acc[FN][FM];
@@ -559,8 +590,7 @@ void tile_kernel(const TileParams p) {
                     const int m = m1 + mi2 * 32 + row, n = n1 + j * 8;
                     u32x4 *to = reinterpret_cast<u32x4 *>(out + (size_t)m * (size_t)ld + n);
                     if (m < p.M && n < ld) {
-                        // dW is not read again here: its stores pass through the caches
-                        if constexpr (AT) __builtin_nontemporal_store(o, to);
+                        if constexpr (EPI == kStream) __builtin_nontemporal_store(o, to);
                         else *to = o;
                     }
                 }
@@ -576,12 +606,7 @@ void tile_kernel(const TileParams p) {
     }
 }
 
-// The largest |grad| of a row with a target (1 without any). dz is stored as
-// its multiple, and the products are scaled back in fp32: with one weight for
-// all rows, as in a mean, the multiple is exactly 1, and -1 at the targets'
-// columns is exact where grad itself would round by the same 2^-9 or so in
-// every row (8192 x 50257 x 4096, mean loss: dH and dW off by 2.6e-3 of their norm,
-// with it 1.9e-3; 1.7e-3 is their own rounding to bf16).
+// peak_of all rows, in one workgroup.
 __global__ __launch_bounds__(1024) void peak_kernel(int M, const int64_t *target, const float *grad, float *peak) {
     __shared__ float s[16];
     float x = 0.0f;
@@ -590,14 +615,13 @@ __global__ __launch_bounds__(1024) void peak_kernel(int M, const int64_t *target
         const float g = fabsf(grad[m]);
         x = fmaxf(x, target[m] >= 0 ? g : 0.0f);
     }
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
+    x = wave_max(x);
     if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
     __syncthreads();
     if (threadIdx.x != 0) return;
 #pragma unroll
     for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
-    *peak = x > 0.0f && x < INFINITY ? x : 1.0f;
+    *peak = peak_of(x);
 }
 
 // Joins a row's parts: lse = log 2 (max + log2 sum_i s_i 2^(m_i - max)). ROWS rows per
@@ -827,8 +851,10 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
     uint16_t *dz = (uint16_t *)ws;
     float *peak = (float *)((char *)ws + b.dz_bytes - 256);
     float *part = (float *)((char *)ws + b.dz_bytes);
-    peak_kernel<<<1, 1024, 0, s>>>(M, target, grad, peak);
-    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return hip_error(e, "peak launch");
+    if (M > kOwnPeakRows) {
+        peak_kernel<<<1, 1024, 0, s>>>(M, target, grad, peak);
+        if (const hipError_t e = hipGetLastError(); e != hipSuccess) return hip_error(e, "peak launch");
+    }
     const uint64_t h_bytes = (uint64_t)M * (uint64_t)K * 2;
     const bool ragged = K % 64 != 0;
     for (int i = 0; i < b.pieces.count; ++i) {
@@ -865,7 +891,14 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         q.R = M;
         q.peak = peak;
         q.C = (uint16_t *)dW + (size_t)c0 * (size_t)K;
-        e = launch_pair<true, true, kStore>(q, plan_pair(kGradWeight, ragged, cols, K, M, true), true, s);
+        // dW is not read again here: its stores pass through the caches. But with
+        // few rows the stores are most of the work, and where rows do not start on
+        // 128-byte lines the caches put the halves of a line together (30 x 100003 x
+        // 1032 backward 229 -> 197 us, 16 x 50257 x 1032 110 -> 102; the other way
+        // round 97 x 58829 x 912 105 -> 114, 16 x 32000 x 4096 171 -> 202)
+        const PairPlan dw = plan_pair(kGradWeight, ragged, cols, K, M, true);
+        e = ragged && M <= kBK ? launch_pair<true, true, kStore>(q, dw, true, s)
+                               : launch_pair<true, true, kStream>(q, dw, true, s);
         if (e != hipSuccess) return hip_error(e, "dW launch");
         // dH += dz W over this piece
         q.B = Wp;

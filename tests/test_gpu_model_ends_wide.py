@@ -1,8 +1,8 @@
-"""The operators at a model's ends on the GPU where an operand's elements lie
-more than 2^31 elements (2^32 bytes) from its first: a long vocabulary, a long
-batch, rows far apart. Cross entropy against fp64 with the bounds of
-test_gpu_model_ends.py; the others bit for bit (exact sums, or the same rows
-packed)."""
+"""More of the operators at a model's ends on the GPU: operands whose elements
+lie more than 2^31 elements (2^32 bytes) from the first (a long vocabulary, a
+long batch, rows far apart), and few rows of the cross entropy. Cross entropy
+against fp64 with the bounds of test_gpu_model_ends.py; the others bit for bit
+(exact sums, or the same rows packed)."""
 from __future__ import annotations
 
 import pytest
@@ -161,3 +161,41 @@ def test_embed_operands_beyond_32_bits(K):
         ref = torch.zeros(V, dy[:, b].shape[1], device="cuda")
         ref.index_add_(0, row, torch.where(inside[:, None], dy[:, b].float() * 0.5, 0.0))
         assert torch.equal(d[:, b], ref.to(bf))
+
+
+# few rows whose weight gradient does not lie on 128-byte lines, in every tile
+# that such a gradient takes (64 x 64, 256 x 192, 192 x 192, 128 x 128), and both
+# sides of the sizes where that ends (64 rows) and where the largest weight takes
+# a launch of its own (256)
+@pytest.mark.parametrize("M,V,K", [(1, 1, 8), (33, 1161, 8200), (16, 4099, 2056), (3, 130, 12296), (64, 20011, 72),
+                                   (65, 20011, 72), (256, 1000, 264), (257, 1000, 264)])
+def test_xent_few_rows(M, V, K):
+    from tests.test_gpu_model_ends import test_xent_every_tile
+    test_xent_every_tile(M, V, K)
+
+
+def test_xent_rows_of_very_different_weight():
+    """The largest weight in the last of 256 rows (of the rows that dz's own
+    workgroups look through): those of the others, 2^20 times smaller, stay
+    whole numbers of bf16 steps of their own."""
+    torch = _torch()
+    M, V, K = 256, 8, 64
+    H = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda")
+    H[:, 0] = 1.0
+    W = torch.zeros(V, K, dtype=torch.bfloat16, device="cuda")
+    W[:, 1] = torch.tensor([1.0, 2.0, 4.0, 8.0, 16.0, 32.0, 64.0, 128.0], device="cuda")
+    t = torch.arange(M, device="cuda") % V
+    lse = torch.full((M,), 3 * 0.6931471805599453, device="cuda")    # 8 equal logits
+    grad = torch.full((M,), 2.0 ** -20, device="cuda")
+    grad[M - 1] = 1.0
+    dH, dW = _nan(M, K, dtype=torch.bfloat16), _nan(V, K, dtype=torch.bfloat16)
+    C.compass_xent_backward(H, W, t, lse, grad, dH, dW, _scratch(C.compass_xent_workspace(M, V, K, backward=True)))
+    g = grad.double()[:, None]
+    p = (0.0 - lse.double()[:, None]).exp().expand(M, V).clone()
+    p[torch.arange(M, device="cuda"), t] -= 1.0
+    dz = g * p
+    err = dz.abs() * U8 + g * 128 * U24
+    w, h = W.double(), H.double()
+    for name, got, ref, e in (("dH", dH, dz @ w, err @ w.abs() + 2 * V * U24 * (dz.abs() @ w.abs())),
+                              ("dW", dW, dz.T @ h, err.T @ h.abs() + 2 * M * U24 * (dz.abs().T @ h.abs()))):
+        _within(name, got, ref, e + U8 * (ref.abs() + e))
