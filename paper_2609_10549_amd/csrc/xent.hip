@@ -427,14 +427,24 @@ void tile_kernel(const TileParams p) {
         const int c0 = n1 + 4 * eq;
         const bool edge = cur.n0 + BN > p.N;
         char *const region = smem + (kPre ? DW * SA : 0) + wave * kRegion;
+        // A row of blocks stays in the accumulators until its turn: the compiler
+        // would else copy all of them to vector registers here, and spill.
+        auto hold = [&](int mi) {
+            if constexpr (kAcc) {
+#pragma unroll
+                for (int ni = 0; ni < FN; ++ni) asm volatile("" : "+a"(acc[ni][mi]));
+            }
+        };
         if constexpr (EPI == kStats) {
             // in units of log 2, so that an exponential is one multiply-add and one
             // v_exp_f32; the maximum is rounded before it is used
             float2 *out = p.parts + (size_t)(2 * cur.tn + (wave & 1)) * (size_t)p.M;
+            const int inside = p.N - c0;   // columns from this lane's first on
 #pragma unroll
             for (int mi = 0; mi < FM; ++mi) {
                 const int m = m1 + mi * 16 + er;
                 float z[FN][4], mx = -INFINITY;
+                hold(mi);
 #pragma unroll
                 for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
@@ -444,7 +454,7 @@ void tile_kernel(const TileParams p) {
                     for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            if (c0 + ni * 16 + e >= p.N) z[ni][e] = -INFINITY;
+                            if (ni * 16 + e >= inside) z[ni][e] = -INFINITY;
                 }
 #pragma unroll
                 for (int ni = 0; ni < FN; ++ni)
@@ -458,16 +468,21 @@ void tile_kernel(const TileParams p) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[ni][e], kLog2e, -sub));
                 sum = row_sum(sum);
+                int t = -1;   // the target's place from this lane's first column
                 if (m < p.M) {
                     if (eq == 0) out[m] = make_float2(mx, sum);
-                    const int64_t t = p.target[m] - p.v0 - c0;
-                    if (t >= 0 && t < WN && t + c0 < p.N) {
+                    const int64_t at = p.target[m] - p.v0 - c0;
+                    if (at >= 0 && at < WN && at < inside) t = (int)at;
+                }
+                if (__ballot(t >= 0)) {   // (a few per cent of the blocks hold a target)
+                    float tz = 0.0f;
+                    bool mine = false;
 #pragma unroll
-                        for (int ni = 0; ni < FN; ++ni)
+                    for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (t == ni * 16 + e) p.tlogit[m] = z[ni][e];
-                    }
+                        for (int e = 0; e < 4; ++e)
+                            if (t == ni * 16 + e) tz = z[ni][e], mine = true;
+                    if (mine) p.tlogit[m] = tz;
                 }
                 __builtin_amdgcn_sched_barrier(0);   // (rows of blocks started together spill)
             }
@@ -547,6 +562,7 @@ void tile_kernel(const TileParams p) {
                     const int mi = 2 * mi2 + h;
                     char *w = region + (er + h * 16) * RB + 8 * (eq & 1);
                     f32x4 x[FN];
+                    hold(mi);
 #pragma unroll
                     for (int ni = 0; ni < FN; ++ni) {
                         x[ni] = acc[ni][mi];
