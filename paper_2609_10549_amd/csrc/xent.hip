@@ -35,7 +35,7 @@ namespace {
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 enum Epilogue : int {
     kStats = 0,   // row maxima and sums of exponentials, the targets' logits
@@ -257,9 +257,9 @@ constexpr int kOwnPeakRows = 256;
 // power allows, 1.35 to 1.42 PFLOP/s (8192 x 50257 x 4096 forward 2.4 ms, its
 // backward 7.2 to 7.5 ms from card to card; MFMA busy 0.66 to 0.74), and what a
 // tile's edges cost beside its stages: 8192 x 50257 x 1024 forward 985 us with a
-// workgroup per tile, 915 with the next tile's loads under the epilogue and
-// exponentials of one multiply-add each. Few rows: W from memory, 8 x 32000 x
-// 4096 44 to 51 us (5.2 to 6.0 TB/s; 38 on the same W again).
+// workgroup per tile, 915 with the next tile's loads under the epilogue. Few
+// rows: W from memory, 8 x 32000 x 4096 44 to 51 us (5.2 to 6.0 TB/s; 38 on the
+// same W again).
 template <int BM, int BN, int DW, bool AT, bool BT, int EPI>
 __global__ __launch_bounds__(kThreads, (160 << 10) / (((DW + 1) * BM + DW * BN) * 128))
 void tile_kernel(const TileParams p) {
@@ -436,8 +436,12 @@ void tile_kernel(const TileParams p) {
             }
         };
         if constexpr (EPI == kStats) {
-            // in units of log 2, so that an exponential is one multiply-add and one
-            // v_exp_f32; the maximum is rounded before it is used
+            // each half's maximum as it is and its sum relative to it: the largest
+            // column's exponential is exactly 1, so that a sum is at least 1 and a
+            // row's lse never below its largest logit. (In units of log 2 an
+            // exponential is one operation less, but lse came back rounded twice at
+            // the logit's size, and certain rows had losses below 0. What it costs:
+            // 4096 x 32000 x 512 148 -> 150 us, 8192 x 50257 x 1024 743 -> 744.)
             float2 *out = p.parts + (size_t)(2 * cur.tn + (wave & 1)) * (size_t)p.M;
             const int inside = p.N - c0;   // columns from this lane's first on
 #pragma unroll
@@ -460,13 +464,13 @@ void tile_kernel(const TileParams p) {
                 for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) mx = fmaxf(mx, z[ni][e]);
-                mx = row_max(mx) * kLog2e;
+                mx = row_max(mx);
                 const float sub = mx == -INFINITY ? 0.0f : mx;   // no column of this half is inside
                 float sum = 0.0f;
 #pragma unroll
                 for (int ni = 0; ni < FN; ++ni)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[ni][e], kLog2e, -sub));
+                    for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((z[ni][e] - sub) * kLog2e);
                 sum = row_sum(sum);
                 int t = -1;   // the target's place from this lane's first column
                 if (m < p.M) {
@@ -640,7 +644,7 @@ __global__ __launch_bounds__(1024) void peak_kernel(int M, const int64_t *target
     *peak = peak_of(x);
 }
 
-// Joins a row's parts: lse = log 2 (max + log2 sum_i s_i 2^(m_i - max)). ROWS rows per
+// Joins a row's parts: lse = max + log sum_i s_i exp(m_i - max). ROWS rows per
 // workgroup, 256 / ROWS threads each: 16 rows read whole 128-byte lines of the
 // parts; few rows (at most 256) take a workgroup each (8 rows of 1000 parts:
 // 20.6 us with 16).
@@ -655,7 +659,7 @@ __global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, con
     float mx = -INFINITY, sum = 0.0f;
     auto add = [&](float2 x) {
         const float top = fmaxf(mx, x.x), sub = top == -INFINITY ? 0.0f : top;
-        sum = sum * __builtin_amdgcn_exp2f(mx - sub) + x.y * __builtin_amdgcn_exp2f(x.x - sub);
+        sum = sum * __builtin_amdgcn_exp2f((mx - sub) * kLog2e) + x.y * __builtin_amdgcn_exp2f((x.x - sub) * kLog2e);
         mx = top;
     };
     if (m < M) {
@@ -672,7 +676,7 @@ __global__ __launch_bounds__(256) void stats_kernel(int M, int V, int parts, con
         }
     }
     if (q != 0 || m >= M) return;
-    const float l = (mx + log2f(sum)) * kLn2;
+    const float l = mx + logf(sum);
     const int64_t t = target[m];
     float tl = 0.0f;
     if (t >= v0 && t - v0 < V) tl = tlogit[m];
