@@ -552,7 +552,7 @@ void tile_kernel(const TileParams p) {
                 for (int mi = 0; mi < FM; ++mi) {
                     const int m = min(m1 + mi * 16 + er, p.M - 1);
                     const int64_t id = p.target[m], at = id - p.v0 - c0;
-                    lse[mi] = p.lse[m] * kLog2e;
+                    lse[mi] = p.lse[m];
                     g[mi] = id < 0 ? 0.0f : p.grad[m] / peak;
                     t[mi] = id < 0 || at < 0 || at >= WN ? -1 : (int)at;
                 }
@@ -573,7 +573,9 @@ void tile_kernel(const TileParams p) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             if constexpr (EPI == kDz) {
-                                const float pr = __builtin_amdgcn_exp2f(__builtin_fmaf(x[ni][e], kLog2e, -lse[mi]));
+                                // (1 where the logit is all of lse: an lse in units of
+                                // log 2 is off by its rounding, and so was 1 - pr)
+                                const float pr = __builtin_amdgcn_exp2f((x[ni][e] - lse[mi]) * kLog2e);
                                 x[ni][e] = g[mi] == 0.0f ? 0.0f : g[mi] * pr;   // (0 whatever the logits are)
                             } else {
                                 x[ni][e] *= peak;

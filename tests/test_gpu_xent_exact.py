@@ -97,3 +97,39 @@ def test_one_column_is_certain_at_any_size(size):
     C.compass_xent_forward(H, W, t, lse, tl, loss, _scratch(C.compass_xent_workspace(M, 1, K)))
     z = H[:, 0].double() + H[:, 1].double()
     assert torch.equal(lse, z.float()) and torch.equal(tl, z.float()) and not loss.any()
+
+
+def _backward(H, W, t, lse, grad):
+    torch = _torch()
+    (M, K), V = H.shape, W.shape[0]
+    dH, dW = _nan(M, K, dtype=torch.bfloat16), _nan(V, K, dtype=torch.bfloat16)
+    C.compass_xent_backward(H, W, t, lse, grad, dH, dW, _scratch(C.compass_xent_workspace(M, V, K, backward=True)))
+    return dH, dW
+
+
+@pytest.mark.parametrize("M,V,K,at", DOMINATED)
+def test_certain_rows_have_no_gradient(M, V, K, at):
+    """exp(z - lse) is 1 where lse is z: what is left of a certain row are the
+    other columns, e^-31 or less each."""
+    print(f"xent dominated backward {M} {V} {K}", flush=True)
+    torch = _torch()
+    H, W, t = _dominated(M, V, K, at, 74, lo=1.0 if V == 1 else 32.0)
+    lse = torch.from_numpy(E.xent_forward(_np(H), _np(W), t.cpu().numpy())[0]).float().cuda()
+    grad = torch.randn(M, generator=torch.Generator().manual_seed(75)).cuda()
+    dH, dW = _backward(H, W, t, lse, grad)
+    if V == 1:
+        assert not dH.any() and not dW.any()
+    left = (V - 1) * float(np.exp(-31.0))
+    assert (dH.abs().amax(1) <= grad.abs() * left).all()
+    assert float(dW.abs().max()) <= float((grad.abs() * H[:, 0]).sum()) * left
+
+
+@pytest.mark.parametrize("size", [8000.0, 2.0 ** 60, 2.0 ** 127])
+def test_one_column_has_no_gradient_at_any_size(size):
+    torch = _torch()
+    M, K = 70, 64
+    H, W, t = _dominated(M, 1, K, 0, 76, lo=size, hi=1.9 * size)
+    H[::2] *= -1
+    lse = (H[:, 0].double() + H[:, 1].double()).float()
+    dH, dW = _backward(H, W, t, lse, torch.ones(M, device="cuda"))
+    assert not dH.any() and not dW.any()
