@@ -361,7 +361,7 @@ __global__ __launch_bounds__(1024) void long_rows_kernel(const Gradient g) {
     for (int e = 0; e < V; ++e) s[w][e * 64 + lane] = f[e];
     __syncthreads();
     if (w != 0) return;
-#pragma unroll
+#pragma unroll 5   // (of V registers each: all 15 at once spill)
     for (int i = 1; i < 16; ++i)
 #pragma unroll
         for (int e = 0; e < V; ++e) f[e] += s[i][e * 64 + lane];

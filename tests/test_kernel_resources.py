@@ -53,7 +53,7 @@ def kernels():
     return found
 
 
-@pytest.mark.parametrize("family", ["tile_kernel", "norm_"])
+@pytest.mark.parametrize("family", ["tile_kernel", "norm_", ""])
 def test_no_kernel_uses_private_memory(kernels, family):
     mine = [k for k in kernels if family in k[".name"]]
     assert mine
