@@ -310,6 +310,8 @@ int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void
  * with a workspace of its own) and all of them may be captured in a HIP graph.
  * A workspace may be used again by the next call on the same stream; its
  * contents need not be initialised. Element types: COMPASS_BF16 or COMPASS_F32.
+ * Vocabulary ids are 64-bit, a shard's first id v0 not negative and v0 + V within
+ * 64 bits; any other id or target lies outside the shard.
  * Argument errors (COMPASS_ERR_INVALID, COMPASS_ERR_UNSUPPORTED) and a device
  * other than gfx950 (COMPASS_ERR_UNSUPPORTED) are found before anything is
  * enqueued; COMPASS_ERR_HIP when a launch fails. All results are the same bits

@@ -55,6 +55,10 @@ struct Cover {
     }
 };
 
+// An id's distance from v0 >= 0, -1 below it (no difference of two 64-bit numbers
+// that wraps round: an id far below zero would come out in the table).
+__device__ __forceinline__ int64_t row_of(int64_t id, int64_t v0) { return id < v0 ? -1 : id - v0; }
+
 // TOKENS tokens per group, their rows in flight together.
 //
 // Bound by memory. 32768 tokens, 50257 x 4096 bf16, token frequencies as
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(Cover cov, int tokens, int 
     int c[TOKENS];
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
-        const int64_t row = t0 + j < tokens ? ids[t0 + j] - v0 : -1;
+        const int64_t row = t0 + j < tokens ? row_of(ids[t0 + j], v0) : -1;
         inside[j] = row >= 0 && row < vocab;
         c[j] = cov.column<V>() - line_shift<LOOSE>(y + (int64_t)(t0 + j) * ldy);
         if (inside[j]) p[j] = load_pack<T, V, LOOSE>(table + row * ldt, c[j], K);
@@ -88,7 +92,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(Cover cov, int tokens, int 
 
 // Table row of a token, `vocab` for ids outside it.
 __device__ __forceinline__ int table_row(int64_t id, int64_t v0, int vocab) {
-    const int64_t r = id - v0;
+    const int64_t r = row_of(id, v0);
     return r >= 0 && r < vocab ? (int)r : vocab;
 }
 
@@ -465,7 +469,8 @@ int op_embed_forward(int T, int V, int K, int type, const int64_t *ids, int64_t 
     int rc = check(T, V, K, type);
     if (rc != COMPASS_OK) return rc;
     if (!ids || !table || !y) return set_error(COMPASS_ERR_INVALID, "ids, table and y are required");
-    if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
+    if (v0 < 0 || v0 > INT64_MAX - V)
+        return set_error(COMPASS_ERR_INVALID, "v0 must not be negative, v0 + V must fit 64 bits");
     if (ldt < K || ldy < K) return set_error(COMPASS_ERR_INVALID, "rows of %d elements overlap", K);
     if (off_element(table, type) || off_element(y, type))
         return set_error(COMPASS_ERR_INVALID, "an operand is not aligned to its elements");
@@ -499,7 +504,8 @@ int op_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *
     if (rc != COMPASS_OK || (rc = check(T, V, K, gtype)) != COMPASS_OK) return rc;
     if (!ids || !dy || !dtable || !ws)
         return set_error(COMPASS_ERR_INVALID, "ids, dy, dtable and the workspace are required");
-    if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
+    if (v0 < 0 || v0 > INT64_MAX - V)
+        return set_error(COMPASS_ERR_INVALID, "v0 must not be negative, v0 + V must fit 64 bits");
     if (ldy < K || ldt < K) return set_error(COMPASS_ERR_INVALID, "rows of %d elements overlap", K);
     if (off_element(dy, dtype) || off_element(dtable, gtype))
         return set_error(COMPASS_ERR_INVALID, "an operand is not aligned to its elements");

@@ -475,7 +475,7 @@ void tile_kernel(const TileParams p) {
                 int t = -1;   // the target's place from this lane's first column
                 if (m < p.M) {
                     if (eq == 0) out[m] = make_float2(mx, sum);
-                    const int64_t at = p.target[m] - p.v0 - c0;
+                    const int64_t id = p.target[m], at = id < p.v0 ? -1 : id - p.v0 - c0;   // (no difference wraps)
                     if (at >= 0 && at < WN && at < inside) t = (int)at;
                 }
                 if (__ballot(t >= 0)) {   // (a few per cent of the blocks hold a target)
@@ -551,10 +551,10 @@ void tile_kernel(const TileParams p) {
 #pragma unroll
                 for (int mi = 0; mi < FM; ++mi) {
                     const int m = min(m1 + mi * 16 + er, p.M - 1);
-                    const int64_t id = p.target[m], at = id - p.v0 - c0;
+                    const int64_t id = p.target[m], at = id < p.v0 ? -1 : id - p.v0 - c0;
                     lse[mi] = p.lse[m];
                     g[mi] = id < 0 ? 0.0f : p.grad[m] / peak;
-                    t[mi] = id < 0 || at < 0 || at >= WN ? -1 : (int)at;
+                    t[mi] = at < 0 || at >= WN ? -1 : (int)at;
                 }
             }
             uint16_t *out = EPI == kDz ? p.dz : p.C;
@@ -809,7 +809,8 @@ int op_xent_forward(int M, int V, int K, const void *H, const void *W, const int
         return set_error(COMPASS_ERR_INVALID, "H, W, target, lse, tlogit and the workspace are required");
     if (misaligned(H) || misaligned(W) || misaligned(ws))
         return set_error(COMPASS_ERR_INVALID, "H, W and the workspace must be 16-byte aligned");
-    if (v0 < 0) return set_error(COMPASS_ERR_INVALID, "v0 must not be negative");
+    if (v0 < 0 || v0 > INT64_MAX - V)
+        return set_error(COMPASS_ERR_INVALID, "v0 must not be negative, v0 + V must fit 64 bits");
     const PairPlan pl = plan_pair(kLogits, K % 64 != 0, M, V, K, false);
     if (ws_bytes < forward_bytes(pl, M))
         return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes, need %zu", ws_bytes, forward_bytes(pl, M));
@@ -862,7 +863,8 @@ int op_xent_backward(int M, int V, int K, const void *H, const void *W, const in
         return set_error(COMPASS_ERR_INVALID, "every operand and the workspace are required");
     if (misaligned(H) || misaligned(W) || misaligned(dH) || misaligned(dW) || misaligned(ws))
         return set_error(COMPASS_ERR_INVALID, "H, W, dH, dW and the workspace must be 16-byte aligned");
-    if (v0 < 0 || piece < 0) return set_error(COMPASS_ERR_INVALID, "v0 and piece must not be negative");
+    if (v0 < 0 || v0 > INT64_MAX - V || piece < 0)
+        return set_error(COMPASS_ERR_INVALID, "v0 and piece must not be negative, v0 + V must fit 64 bits");
     const BackwardPlan b = plan_backward(M, V, K, piece);
     if ((rc = check_piece(M, b)) != COMPASS_OK) return rc;
     if (ws_bytes < b.dz_bytes + b.part_bytes)
