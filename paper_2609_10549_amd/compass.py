@@ -124,37 +124,37 @@ _SIGS = {
                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
     "compass_transfer": (ctypes.c_int, [ctypes.POINTER(compass_problem), ctypes.POINTER(compass_links), ctypes.c_void_p]),
     "compass_sequential": (ctypes.c_int, [ctypes.POINTER(compass_problem), ctypes.POINTER(compass_links), ctypes.c_void_p]),
-        "compass_xent_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                            ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
-        "compass_xent_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
-                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
-                                          ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
-                                          ctypes.c_void_p]),
-        "compass_xent_join": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
-                                       ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
-        "compass_xent_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
-                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
-                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
-                                           ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
-        "compass_norm_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                          ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
-                                          ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
-                                          ctypes.c_void_p, ctypes.c_void_p]),
-        "compass_norm_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
-        "compass_norm_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
-                                           ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
-                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
-                                           ctypes.c_size_t, ctypes.c_void_p]),
-        "compass_embed_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
-                                           ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
-        "compass_embed_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                             ctypes.POINTER(ctypes.c_size_t)]),
-        "compass_embed_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
-                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
-                                            ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
-                                            ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "compass_xent_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                              ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_xent_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                            ctypes.c_void_p]),
+    "compass_xent_join": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "compass_xent_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                             ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "compass_norm_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                            ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p,
+                                            ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_void_p, ctypes.c_void_p]),
+    "compass_norm_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_norm_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                             ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                             ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                             ctypes.c_size_t, ctypes.c_void_p]),
+    "compass_embed_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                             ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64,
+                                             ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "compass_embed_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                               ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_embed_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                              ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                              ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
+                                              ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "compass_sync": (ctypes.c_int, []),
     "compass_kernel_times": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int]),
     "compass_tile_trace": (ctypes.c_int, [ctypes.POINTER(ctypes.c_uint32), ctypes.c_int]),
@@ -409,9 +409,10 @@ def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False):
     """The address of x, a GPU tensor of the given shape whose dtype is one of
     `kinds`, contiguous or, with `rows`, in rows of consecutive elements that do
     not overlap; ValueError for any other. None and plain int addresses pass as
-    they are, the latter on the caller's responsibility. (One call per operand
-    for the check and the address: a single-token operator takes as long on the
-    host as on the GPU.)"""
+    they are, the latter on the caller's responsibility; operands whose sizes,
+    type or rows are read, and workspaces, must be tensors (_dims, _rows, _ws). (One
+    call per operand for the check and the address: a single-token operator takes
+    as long on the host as on the GPU.)"""
     if x is None or isinstance(x, int):
         return x
     if x.shape == shape and x.dtype in kinds and x.is_cuda and (
@@ -427,17 +428,39 @@ def _typed(x, what: str, shape: tuple, kinds: tuple, rows: bool = False):
     raise ValueError(f"{what}: must be contiguous" + (" within rows" if rows else ""))
 
 
+def _not_a_tensor(what: str) -> ValueError:
+    return ValueError(f"{what}: must be a tensor (its sizes are read)")
+
+
+def _dims(x, what: str, n: int = 2) -> tuple:
+    """The sizes of x, a tensor of n dimensions."""
+    try:
+        shape = x.shape
+    except AttributeError:
+        raise _not_a_tensor(what) from None
+    if len(shape) != n:
+        raise ValueError(f"{what}: shape {_shape_of(x)}, expected {n} dimensions")
+    return shape
+
+
 def _kind(x) -> int:
     return F32 if x.element_size() == 4 else BF16
 
 
-def _ld(x) -> int:
-    return x.stride(0) if x.shape[0] > 1 else x.shape[1]
+def _rows(x, what: str, shape: tuple, kinds: tuple) -> tuple:
+    """Address of a tensor as in _typed with `rows`, and the elements from one of
+    its rows to the next."""
+    at = _typed(x, what, shape, kinds, True)
+    try:
+        ld = x.stride(0)
+    except AttributeError:
+        raise _not_a_tensor(what) from None
+    return at, ld if shape[0] > 1 else shape[1]
 
 
 def _ws(x) -> tuple:
     """Address and bytes of a workspace."""
-    if x is None or not x.is_cuda or not x.is_contiguous():
+    if x is None or isinstance(x, int) or not x.is_cuda or not x.is_contiguous():
         raise ValueError("workspace: must be a contiguous GPU tensor")
     return x.data_ptr(), x.nbytes
 
@@ -454,8 +477,8 @@ def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0
     """lse, tlogit and loss (M each, fp32; loss may be None) of hidden states H
     (M x K) and the vocabulary rows W (V x K) from id v0; see the header."""
     k = _kinds or _find_kinds()
-    M, K = H.shape
-    V = W.shape[0]
+    M, K = _dims(H, "H")
+    V = _dims(W, "W")[0]
     rc = (_lib or lib()).compass_xent_forward(
         M, V, K, _typed(H, "H", (M, K), k.bits), _typed(W, "W", (V, K), k.bits), _typed(target, "target", (M,), k.index),
         v0, _typed(lse, "lse", (M,), k.float), _typed(tlogit, "tlogit", (M,), k.float),
@@ -467,7 +490,7 @@ def compass_xent_forward(H, W, target, lse, tlogit, loss, workspace, v0: int = 0
 def compass_xent_join(lse_parts, tlogit_parts, target, lse, loss, stream=None) -> None:
     """lse and loss of the whole vocabulary from the n ranks' shards (n x M)."""
     k = _kinds or _find_kinds()
-    n, M = lse_parts.shape
+    n, M = _dims(lse_parts, "lse_parts")
     rc = (_lib or lib()).compass_xent_join(
         n, M, _typed(lse_parts, "lse_parts", (n, M), k.float), _typed(tlogit_parts, "tlogit_parts", (n, M), k.float),
         _typed(target, "target", (M,), k.index), _typed(lse, "lse", (M,), k.float), _typed(loss, "loss", (M,), k.float),
@@ -480,8 +503,8 @@ def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 
                           stream=None) -> None:
     """Gradients dH (M x K) and dW (V x K) of sum(grad * loss); see the header."""
     k = _kinds or _find_kinds()
-    M, K = H.shape
-    V = W.shape[0]
+    M, K = _dims(H, "H")
+    V = _dims(W, "W")[0]
     rc = (_lib or lib()).compass_xent_backward(
         M, V, K, _typed(H, "H", (M, K), k.bits), _typed(W, "W", (V, K), k.bits), _typed(target, "target", (M,), k.index),
         v0, _typed(lse, "lse", (M,), k.float), _typed(grad, "grad", (M,), k.float), _typed(dH, "dH", (M, K), k.bits),
@@ -493,23 +516,25 @@ def compass_xent_backward(H, W, target, lse, grad, dH, dW, workspace, v0: int = 
 def _params(gamma, beta, N: int, kinds: tuple) -> tuple:
     """The addresses and the type of the norm's parameters (either may be None)."""
     g, b = _typed(gamma, "gamma", (N,), kinds), _typed(beta, "beta", (N,), kinds)
-    if gamma is None:
-        return g, b, F32 if beta is None else _kind(beta)
-    if beta is not None and gamma.dtype != beta.dtype:
-        raise ValueError(f"gamma and beta: {gamma.dtype} and {beta.dtype}, expected one type")
-    return g, b, _kind(gamma)
+    try:
+        if gamma is None:
+            return g, b, F32 if beta is None else _kind(beta)
+        if beta is not None and gamma.dtype != beta.dtype:
+            raise ValueError(f"gamma and beta: {gamma.dtype} and {beta.dtype}, expected one type")
+        return g, b, _kind(gamma)
+    except AttributeError:
+        raise ValueError("gamma, beta: must be tensors (their type is read)") from None
 
 
 def compass_norm_forward(x, gamma, beta, y, mean, rstd, eps: float = 1e-5, stream=None) -> None:
     """Layer norm y (M x N, of x's type) with its statistics mean and rstd (M,
     fp32); gamma and beta may be None. Rows of x and y may lie apart."""
     k = _kinds or _find_kinds()
-    shape = M, N = x.shape
+    shape = M, N = _dims(x, "x")
     g, b, ptype = _params(gamma, beta, N, k.elements)
     rc = (_lib or lib()).compass_norm_forward(
-        M, N, _kind(x), ptype, _typed(x, "x", shape, k.elements, True), _ld(x), g, b, eps,
-        _typed(y, "y", shape, (x.dtype,), True), _ld(y), _typed(mean, "mean", (M,), k.float),
-        _typed(rstd, "rstd", (M,), k.float), _stream(stream))
+        M, N, _kind(x), ptype, *_rows(x, "x", shape, k.elements), g, b, eps, *_rows(y, "y", shape, (x.dtype,)),
+        _typed(mean, "mean", (M,), k.float), _typed(rstd, "rstd", (M,), k.float), _stream(stream))
     if rc < 0:
         _check(rc, "compass_norm_forward")
 
@@ -525,14 +550,14 @@ def compass_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace
     """dx (of x's type), dgamma and dbeta (N, fp32; None: not wanted) of
     compass_norm_forward; gamma may be None."""
     k = _kinds or _find_kinds()
-    shape = M, N = x.shape
+    shape = M, N = _dims(x, "x")
     kind = (x.dtype,)
     g, _, ptype = _params(gamma, None, N, k.elements)
     rc = (_lib or lib()).compass_norm_backward(
-        M, N, _kind(x), ptype, _typed(dy, "dy", shape, kind, True), _ld(dy), _typed(x, "x", shape, k.elements, True),
-        _ld(x), g, _typed(mean, "mean", (M,), k.float), _typed(rstd, "rstd", (M,), k.float),
-        _typed(dx, "dx", shape, kind, True), _ld(dx), _typed(dgamma, "dgamma", (N,), k.float),
-        _typed(dbeta, "dbeta", (N,), k.float), *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+        M, N, _kind(x), ptype, *_rows(dy, "dy", shape, kind), *_rows(x, "x", shape, k.elements), g,
+        _typed(mean, "mean", (M,), k.float), _typed(rstd, "rstd", (M,), k.float), *_rows(dx, "dx", shape, kind),
+        _typed(dgamma, "dgamma", (N,), k.float), _typed(dbeta, "dbeta", (N,), k.float),
+        *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
     if rc < 0:
         _check(rc, "compass_norm_backward")
 
@@ -541,11 +566,11 @@ def compass_embed_forward(ids, table, y, scale: float = 1.0, v0: int = 0, stream
     """y[t] = scale * table[ids[t] - v0] (T x K, of the table's type), zeros for
     ids outside the table's rows."""
     k = _kinds or _find_kinds()
-    shape = V, K = table.shape
-    T = ids.shape[0]
+    shape = V, K = _dims(table, "table")
+    T = _dims(ids, "ids", 1)[0]
     rc = (_lib or lib()).compass_embed_forward(
-        T, V, K, _kind(table), _typed(ids, "ids", (T,), k.index), v0, _typed(table, "table", shape, k.elements, True),
-        _ld(table), scale, _typed(y, "y", (T, K), (table.dtype,), True), _ld(y), _stream(stream))
+        T, V, K, _kind(table), _typed(ids, "ids", (T,), k.index), v0, *_rows(table, "table", shape, k.elements), scale,
+        *_rows(y, "y", (T, K), (table.dtype,)), _stream(stream))
     if rc < 0:
         _check(rc, "compass_embed_forward")
 
@@ -562,12 +587,12 @@ def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: i
     """dtable (V x K) of compass_embed_forward from dy (T x K); with accumulate,
     added to what dtable holds."""
     k = _kinds or _find_kinds()
-    T, K = dy.shape
-    V = dtable.shape[0]
+    T, K = _dims(dy, "dy")
+    V = _dims(dtable, "dtable")[0]
     rc = (_lib or lib()).compass_embed_backward(
         T, V, K, _kind(dy), _kind(dtable), _typed(ids, "ids", (T,), k.index), v0,
-        _typed(dy, "dy", (T, K), k.elements, True), _ld(dy), scale, _typed(dtable, "dtable", (V, K), k.elements, True),
-        _ld(dtable), 1 if accumulate else 0, *_ws(workspace), _stream(stream))
+        *_rows(dy, "dy", (T, K), k.elements), scale, *_rows(dtable, "dtable", (V, K), k.elements),
+        1 if accumulate else 0, *_ws(workspace), _stream(stream))
     if rc < 0:
         _check(rc, "compass_embed_backward")
 
