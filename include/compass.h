@@ -311,7 +311,8 @@ int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void
  * A workspace may be used again by the next call on the same stream; its
  * contents need not be initialised. Element types: COMPASS_BF16 or COMPASS_F32.
  * Vocabulary ids are 64-bit, a shard's first id v0 not negative and v0 + V within
- * 64 bits; any other id or target lies outside the shard.
+ * 64 bits; any other id or target lies outside the shard. M, V, K, N and T
+ * are at least 1: a rank without tokens makes no call.
  * Argument errors (COMPASS_ERR_INVALID, COMPASS_ERR_UNSUPPORTED) and a device
  * other than gfx950 (COMPASS_ERR_UNSUPPORTED) are found before anything is
  * enqueued; COMPASS_ERR_HIP when a launch fails. All results are the same bits
@@ -326,7 +327,8 @@ int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void
  * (0 when the target is not in the shard), loss[m] = lse[m] - tlogit[m]. The
  * logits are never stored. target: M ids of the whole vocabulary, 64-bit; a row
  * with a negative target has loss 0 and gradient 0. Products accumulate in
- * fp32; lse, tlogit and loss are fp32.
+ * fp32; lse, tlogit and loss are fp32. lse is not below the row's largest logit,
+ * so a final loss is not negative.
  *
  * compass_xent_workspace: bytes of the workspace of compass_xent_forward
  *   (backward = 0) or of compass_xent_backward with this `piece` (backward = 1).
@@ -338,7 +340,8 @@ int compass_gemm_noalloc(int M, int N, int K, const void *A, const void *W, void
  * compass_xent_backward: with the whole vocabulary's lse and grad[m] the
  *   derivative of the final result by loss[m],
  *     dz[m][v] = grad[m] (exp(z[m][v] - lse[m]) - [v0 + v = target[m]])
- *   dH = dz W (M x K bf16, this shard's share: to be summed over the ranks) and
+ *   dH = dz W (M x K bf16, this shard's share: to be summed over the ranks, each
+ *   share rounded once, at most 2^-8 of its elements) and
  *   dW = dz^T H (V x K bf16). z is computed again, dz held in bf16 (it enters
  *   the matrix cores in that type: at most 2^-8 relative per element, which
  *   does not accumulate) for one piece of `piece` vocabulary rows at a time (0: the
@@ -384,7 +387,8 @@ int compass_norm_backward(int M, int N, int dtype, int ptype, const void *dy, in
  * gtype. accumulate = 0 writes every row of dtable; accumulate = 1 adds to the
  * rows that have tokens and leaves the others untouched (a table tied to the
  * output weight, whose gradient compass_xent_backward wrote). Limits: T up to
- * 2^20, V up to 2^24, K up to 2^20. */
+ * 2^20, V up to 2^24, K up to 2^20. The gradient sorts the tokens, in a time that
+ * grows with T^2 (MI355X: 0.03 ms for 2^16 tokens, 3.3 ms for 2^20). */
 int compass_embed_forward(int T, int V, int K, int dtype, const int64_t *ids, int64_t v0, const void *table,
                           int64_t ldt, float scale, void *y, int64_t ldy, void *stream);
 int compass_embed_workspace(int T, int V, int K, size_t *bytes);

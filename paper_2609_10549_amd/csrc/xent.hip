@@ -254,12 +254,12 @@ constexpr int kOwnPeakRows = 256;
 // runs (the epilogue's LDS is then the buffer that those stages leave free).
 //
 // What bounds it: the large tiles, the matrix cores at the clock the chip's
-// power allows, 1.35 to 1.42 PFLOP/s (8192 x 50257 x 4096 forward 2.4 ms, its
-// backward 7.2 to 7.5 ms from card to card; MFMA busy 0.66 to 0.74), and what a
-// tile's edges cost beside its stages: 8192 x 50257 x 1024 forward 985 us with a
-// workgroup per tile, 915 with the next tile's loads under the epilogue. Few
-// rows: W from memory, 8 x 32000 x 4096 44 to 51 us (5.2 to 6.0 TB/s; 38 on the
-// same W again).
+// power allows, 1.35 to 1.45 PFLOP/s (8192 x 50257 x 4096 forward 2.33 to 2.37 ms, its
+// backward 7.3 to 7.6 ms from card to card; MFMA busy 0.66 to 0.74), and what a
+// tile's edges cost beside its stages: 8192 x 50257 x 1024 forward went from 985 us
+// with a workgroup per tile to 915 with the next tile's loads under the epilogue
+// (799 now). Few rows: W from memory, 8 x 32000 x 4096 44 to 51 us (5.2 to 6.0 TB/s;
+// 38 on the same W again).
 template <int BM, int BN, int DW, bool AT, bool BT, int EPI>
 __global__ __launch_bounds__(kThreads, (160 << 10) / (((DW + 1) * BM + DW * BN) * 128))
 void tile_kernel(const TileParams p) {
@@ -428,7 +428,9 @@ void tile_kernel(const TileParams p) {
         const bool edge = cur.n0 + BN > p.N;
         char *const region = smem + (kPre ? DW * SA : 0) + wave * kRegion;
         // A row of blocks stays in the accumulators until its turn: the compiler
-        // would else copy all of them to vector registers here, and spill.
+        // would else copy all of them to vector registers here, and spill (the
+        // statistics of 256 x 256 tiles: 43 registers, 34 MB written where now 3
+        // are, 8192 x 6283 x 12288 924 -> 916 us).
         auto hold = [&](int mi) {
             if constexpr (kAcc) {
 #pragma unroll
@@ -441,7 +443,7 @@ void tile_kernel(const TileParams p) {
             // row's lse never below its largest logit. (In units of log 2 an
             // exponential is one operation less, but lse came back rounded twice at
             // the logit's size, and certain rows had losses below 0. What it costs:
-            // 4096 x 32000 x 512 148 -> 150 us, 8192 x 50257 x 1024 743 -> 744.)
+            // 4096 x 32000 x 512 148 -> 150 us, 8192 x 50257 x 1024 792 -> 799.)
             float2 *out = p.parts + (size_t)(2 * cur.tn + (wave & 1)) * (size_t)p.M;
             const int inside = p.N - c0;   // columns from this lane's first on
 #pragma unroll

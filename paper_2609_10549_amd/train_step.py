@@ -108,7 +108,8 @@ class Model:
         C.compass_embed_backward(ids, self.dx0, g["E"], self.ws, scale=self.scale, accumulate=True)
         return g
 
-    def step(self, ids, target, lr: float) -> float:
+    def step(self, ids, target, lr: float):
+        """One update; the mean loss before it, on the GPU."""
         loss = self.forward(ids, target).sum() / (target >= 0).sum().clamp(min=1)
         for k, d in self.backward(ids, target).items():
             self.momentum[k].mul_(0.9).add_(d.float())

@@ -3,10 +3,11 @@ metadata: none may use private memory (spilled registers), for which the runtime
 would have to provide scratch behind a call that allocates nothing."""
 import struct
 
-import msgpack
 import pytest
 
 from paper_2609_10549_amd import compass as C
+
+msgpack = pytest.importorskip("msgpack")
 
 MAGIC = b"__CLANG_OFFLOAD_BUNDLE__"
 
