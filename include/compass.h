@@ -396,6 +396,76 @@ int compass_embed_backward(int T, int V, int K, int dtype, int gtype, const int6
                            int64_t ldy, float scale, void *dtable, int64_t ldt, int accumulate, void *workspace,
                            size_t workspace_bytes, void *stream);
 
+/* ---- the MLP in 8 bits ------------------------------------------------------
+ * The norm before the products, the products, and what the backward pass reads
+ * of them. Same conventions as the operators above: device pointers, caller-owned
+ * workspaces, no allocation, no state, any stream, graph capture, the same bits
+ * on every call. Sizes are at least 1; no operand may overlap another except where
+ * it is said.
+ *
+ * 8-bit rows: R rows of n values are R x n bytes of e4m3 (1 sign, 4 exponent, 3
+ * fraction bits, largest 448, no infinity), 16-byte aligned, and R x S bytes of
+ * scales, 4-byte aligned, S = compass_fp8_scale_cols(n) = 4 ceil(n / 512). Values
+ * [128 g, 128 g + 128) of a row share scale byte g, which stands for 2^(byte -
+ * 127); 255 stands for NaN. The operators below that write 8-bit rows take the
+ * smallest byte that brings the largest finite magnitude of the group to at most
+ * 448 (0 for a group of zeros), round each value once to nearest even, turn values
+ * that are not finite to NaN, and write 127 to the bytes behind the last group.
+ * A scale for a block of 128 x 128 of a weight is the same byte in 128 rows. */
+int compass_fp8_scale_cols(int n, int *cols);
+
+/* x (M rows of K elements of type dtype, ldx apart) to 8-bit rows: across = 0, M
+ * rows of K values; across = 1, the transposed, K rows of M values (groups along
+ * M): a weight for the product of its backward pass. And back: x rounded once to
+ * dtype; in bf16 a value as the operators here write it is exact down to 2^-126.
+ * M up to 2^21, K up to 2^17. */
+int compass_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across, void *x8, void *scale,
+                      void *stream);
+int compass_fp8_dequant(int M, int K, int dtype, const void *x8, const void *scale, void *x, int64_t ldx,
+                        void *stream);
+
+/* Root-mean-square norm of the residual stream, over M rows (at most 2^21) of N
+ * elements (at most 16384):
+ *   h = x + residual (rounded to dtype; x itself where residual and h are NULL),
+ *   rstd = 1 / sqrt(sum h^2 / N + eps),  y = h rstd gamma
+ * x, residual, h, y: rows of type dtype, ld elements apart (>= N); gamma: N elements of
+ * type ptype, or NULL (ones); rstd: M fp32. y and the 8-bit rows y8 with scale
+ * (M rows of N values) are both rounded from the fp32 result; either may be NULL.
+ * h may be x or residual, and y may be x or residual where it is not h. Backward, from
+ * h as stored (x where there was no residual), dy = the gradient of y and dh = that of
+ * h from elsewhere (NULL: none), with hh = h rstd and a = dy gamma:
+ *   dx = dh + rstd (a - hh sum(a hh) / N), the gradient of x and of residual,
+ *   dgamma = sum over rows of dy hh (N fp32; NULL: not wanted, and no workspace is needed).
+ * dx may be dy, h or dh. All sums are fp32. */
+int compass_rms_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *residual,
+                        int64_t ldr, const void *gamma, float eps, void *h, int64_t ldh, void *y, int64_t ldy,
+                        void *y8, void *scale, float *rstd, void *stream);
+int compass_rms_workspace(int M, int N, size_t *bytes);
+int compass_rms_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *h, int64_t ldh,
+                         const void *dh, int64_t lddh, const void *gamma, const float *rstd, void *dx, int64_t lddx,
+                         float *dgamma, void *workspace, size_t workspace_bytes, void *stream);
+
+/* C = A W^T of 8-bit rows A (M rows of K values) and W (N rows of K values), each
+ * with its scales: the product of the values they stand for, accumulated in fp32,
+ * rounded once to bf16 (C: M x N, packed, 16-byte aligned). (The matrix core aligns
+ * the products of 8 consecutive k to the largest of the 8 and cuts them at 2^-13 of
+ * its binade, far below the values' own 2^-4; nothing else is lost before fp32.) With dY and the
+ * transposed weight in 8-bit rows it is the gradient of the activation. K a
+ * multiple of 16 up to 2^17, M and N up to 2^20. */
+int compass_fp8_gemm_workspace(int M, int N, int K, size_t *bytes);
+int compass_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const void *W, const void *W_scale,
+                     void *C, void *workspace, size_t workspace_bytes, void *stream);
+
+/* dW = dY^T X, a weight's gradient from the activation that the forward pass kept
+ * in 8-bit rows X8 (M rows of K values; compass_rms_forward's y8, compass_fp8_quant's
+ * x8): dY M x N bf16, dW N x K of type gtype, packed and 16-byte aligned. The values
+ * enter the matrix cores in bf16 (exact down to 2^-126), products accumulate in fp32.
+ * accumulate = 1 adds to dW what it holds before the one rounding. N a multiple of 8,
+ * K of 16; M and N up to 2^20, K up to 2^17. */
+int compass_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes);
+int compass_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X8, const void *X_scale, void *dW,
+                      int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Wait until the copy side of every enqueued operator has finished and the
  * device is idle; return the pending asynchronous status (COMPASS_OK or
  * COMPASS_ERR_TIMEOUT) and clear it. COMPASS_ERR_IN_FLIGHT (not cleared) when

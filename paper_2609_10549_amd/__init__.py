@@ -13,6 +13,13 @@ from .compass import (  # noqa: F401
     compass_embed_forward,
     compass_embed_workspace,
     compass_embed_backward,
+    compass_fp8_dequant,
+    compass_fp8_gemm,
+    compass_fp8_gemm_workspace,
+    compass_fp8_quant,
+    compass_fp8_scale_cols,
+    compass_fp8_wgrad,
+    compass_fp8_wgrad_workspace,
     compass_gemm,
     compass_gemm_rs,
     compass_kernel_times,
@@ -28,6 +35,9 @@ from .compass import (  # noqa: F401
     compass_model_t_decomp,
     compass_model_t_fusion,
     compass_pick_strategy,
+    compass_rms_forward,
+    compass_rms_workspace,
+    compass_rms_backward,
     compass_schedule,
     compass_sequential,
     compass_set_option,

@@ -155,6 +155,32 @@ _SIGS = {
                                               ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
                                               ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_int64,
                                               ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
+    "compass_rms_forward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_float, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                           ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p]),
+    "compass_rms_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_rms_backward": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                            ctypes.c_int64, ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p,
+                                            ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                            ctypes.c_int64, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t,
+                                            ctypes.c_void_p]),
+    "compass_fp8_scale_cols": (ctypes.c_int, [ctypes.c_int, ctypes.POINTER(ctypes.c_int)]),
+    "compass_fp8_quant": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_int64,
+                                         ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p]),
+    "compass_fp8_dequant": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                           ctypes.c_void_p, ctypes.c_int64, ctypes.c_void_p]),
+    "compass_fp8_gemm_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                  ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_fp8_gemm": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p,
+                                        ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
+                                        ctypes.c_size_t, ctypes.c_void_p]),
+    "compass_fp8_wgrad_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                   ctypes.POINTER(ctypes.c_size_t)]),
+    "compass_fp8_wgrad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_void_p,
+                                         ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int,
+                                         ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]),
     "compass_sync": (ctypes.c_int, []),
     "compass_kernel_times": (ctypes.c_int, [ctypes.POINTER(ctypes.c_double), ctypes.c_int]),
     "compass_tile_trace": (ctypes.c_int, [ctypes.POINTER(ctypes.c_uint32), ctypes.c_int]),
@@ -385,7 +411,8 @@ def compass_gemm_noalloc(A, W, C, P=None, stream=None) -> None:
 # ------------------------------------------- the ends of a model (see the header)
 class _Kinds:
     """The dtypes of operands: bf16 values as bf16 or as raw patterns, elements
-    of operators of either type, fp32, indices."""
+    of operators of either type, fp32, indices, 8-bit values and their scales
+    (both also as raw patterns)."""
 
     def __init__(self):
         import torch
@@ -393,6 +420,8 @@ class _Kinds:
         self.elements = (torch.bfloat16, torch.float32)
         self.float = (torch.float32,)
         self.index = (torch.int64,)
+        self.eight = (torch.float8_e4m3fn, torch.uint8)
+        self.scale = (torch.uint8, torch.float8_e8m0fnu)
 
 
 _kinds = None
@@ -595,6 +624,127 @@ def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: i
         1 if accumulate else 0, *_ws(workspace), _stream(stream))
     if rc < 0:
         _check(rc, "compass_embed_backward")
+
+
+# ---------------------------------------------- the MLP in 8 bits (see the header)
+def compass_fp8_scale_cols(n: int) -> int:
+    """Bytes of the scales of a row of n 8-bit values."""
+    out = ctypes.c_int()
+    _check(lib().compass_fp8_scale_cols(n, ctypes.byref(out)), "compass_fp8_scale_cols")
+    return out.value
+
+
+def _eight(x, scale, what: str, shape: tuple, k: _Kinds) -> tuple:
+    """The addresses of 8-bit rows and of their scales."""
+    return (_typed(x, what, shape, k.eight),
+            _typed(scale, f"{what}'s scale", (shape[0], 4 * -(-shape[1] // 512)), k.scale))
+
+
+def _sizes(name: str, *sizes) -> int:
+    out = ctypes.c_size_t()
+    _check(getattr(lib(), name)(*sizes, ctypes.byref(out)), name)
+    return out.value
+
+
+def compass_fp8_quant(x, x8, scale, across: bool = False, stream=None) -> None:
+    """8-bit rows x8 with their scales from x (M x K, bf16 or fp32, whose rows may
+    lie apart): M rows of K values, with across the transposed, K rows of M."""
+    k = _kinds or _find_kinds()
+    shape = M, K = _dims(x, "x")
+    rc = (_lib or lib()).compass_fp8_quant(
+        M, K, _kind(x), *_rows(x, "x", shape, k.elements), 1 if across else 0,
+        *_eight(x8, scale, "x8", (K, M) if across else (M, K), k), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_fp8_quant")
+
+
+def compass_fp8_dequant(x8, scale, x, stream=None) -> None:
+    """x (M x K, bf16 or fp32, whose rows may lie apart) = the values that the 8-bit
+    rows x8 with their scales stand for."""
+    k = _kinds or _find_kinds()
+    shape = M, K = _dims(x, "x")
+    at, ld = _rows(x, "x", shape, k.elements)
+    rc = (_lib or lib()).compass_fp8_dequant(M, K, _kind(x), *_eight(x8, scale, "x8", shape, k), at, ld,
+                                             _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_fp8_dequant")
+
+
+def compass_rms_forward(x, gamma, y, rstd, residual=None, h=None, y8=None, scale=None, eps: float = 1e-5,
+                        stream=None) -> None:
+    """Root-mean-square norm of h = x + residual (M x N): h and y of x's type, y8 with
+    scale in 8-bit rows, rstd (M, fp32). Without residual and h the norm is of x; y
+    or y8 may be None; gamma may be None. Rows but y8's may lie apart."""
+    k = _kinds or _find_kinds()
+    shape = M, N = _dims(x, "x")
+    g, _, ptype = _params(gamma, None, N, k.elements)
+    kind, none = (x.dtype,), (None, 0)
+    rc = (_lib or lib()).compass_rms_forward(
+        M, N, _kind(x), ptype, *_rows(x, "x", shape, k.elements),
+        *(none if residual is None else _rows(residual, "residual", shape, kind)), g, eps,
+        *(none if h is None else _rows(h, "h", shape, kind)), *(none if y is None else _rows(y, "y", shape, kind)),
+        *(none if y8 is None and scale is None else _eight(y8, scale, "y8", shape, k)),
+        _typed(rstd, "rstd", (M,), k.float), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_rms_forward")
+
+
+def compass_rms_workspace(M: int, N: int) -> int:
+    """Bytes of the workspace of compass_rms_backward."""
+    return _sizes("compass_rms_workspace", M, N)
+
+
+def compass_rms_backward(dy, h, gamma, rstd, dx, dgamma, workspace, dh=None, stream=None) -> None:
+    """dx (of h's type), the gradient of x and of residual, and dgamma (N, fp32;
+    None: not wanted) of compass_rms_forward; dh: the gradient of h from elsewhere."""
+    k = _kinds or _find_kinds()
+    shape = M, N = _dims(h, "h")
+    kind = (h.dtype,)
+    g, _, ptype = _params(gamma, None, N, k.elements)
+    rc = (_lib or lib()).compass_rms_backward(
+        M, N, _kind(h), ptype, *_rows(dy, "dy", shape, kind), *_rows(h, "h", shape, k.elements),
+        *((None, 0) if dh is None else _rows(dh, "dh", shape, kind)), g, _typed(rstd, "rstd", (M,), k.float),
+        *_rows(dx, "dx", shape, kind), _typed(dgamma, "dgamma", (N,), k.float),
+        *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_rms_backward")
+
+
+def compass_fp8_gemm_workspace(M: int, N: int, K: int) -> int:
+    """Bytes of the workspace of compass_fp8_gemm (0: None will do)."""
+    return _sizes("compass_fp8_gemm_workspace", M, N, K)
+
+
+def compass_fp8_gemm(A, A_scale, W, W_scale, C, workspace, stream=None) -> None:
+    """C (M x N bf16) = A W^T of 8-bit rows A (M x K) and W (N x K)."""
+    k = _kinds or _find_kinds()
+    shape = M, K = _dims(A, "A")
+    N = _dims(W, "W")[0]
+    rc = (_lib or lib()).compass_fp8_gemm(
+        M, N, K, *_eight(A, A_scale, "A", shape, k), *_eight(W, W_scale, "W", (N, K), k),
+        _typed(C, "C", (M, N), k.bits), *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_fp8_gemm")
+
+
+def compass_fp8_wgrad_workspace(M: int, N: int, K: int) -> int:
+    """Bytes of the workspace of compass_fp8_wgrad (0: None will do)."""
+    return _sizes("compass_fp8_wgrad_workspace", M, N, K)
+
+
+def compass_fp8_wgrad(dY, X8, X_scale, dW, workspace, accumulate: bool = False, stream=None) -> None:
+    """dW (N x K, bf16 or fp32) = dY^T X from dY (M x N bf16) and the 8-bit rows X8
+    (M x K); with accumulate, added to what dW holds."""
+    k = _kinds or _find_kinds()
+    M, N = _dims(dY, "dY")
+    K = _dims(X8, "X8")[1]
+    _dims(dW, "dW")
+    rc = (_lib or lib()).compass_fp8_wgrad(
+        M, N, K, _kind(dW), _typed(dY, "dY", (M, N), k.bits), *_eight(X8, X_scale, "X8", (M, K), k),
+        _typed(dW, "dW", (N, K), k.elements), 1 if accumulate else 0,
+        *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+    if rc < 0:
+        _check(rc, "compass_fp8_wgrad")
 
 
 def compass_transfer(problem: Problem, lk: compass_links | None = None, stream=None) -> None:

@@ -91,6 +91,56 @@ int compass_embed_backward(int T, int V, int K, int dtype, int gtype, const int6
                              workspace_bytes, stream);
 }
 
+int compass_rms_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *residual, int64_t
+                        ldr, const void *gamma, float eps, void *h, int64_t ldh, void *y, int64_t ldy, void *y8, void
+                        *scale, float *rstd, void *stream) {
+    return op_rms_forward(M, N, dtype, ptype, x, ldx, residual, ldr, gamma, eps, h, ldh, y, ldy, y8, scale, rstd,
+                          stream);
+}
+
+int compass_rms_workspace(int M, int N, size_t *bytes) {
+    return op_rms_workspace(M, N, bytes);
+}
+
+int compass_rms_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *h, int64_t ldh,
+                         const void *dh, int64_t lddh, const void *gamma, const float *rstd, void *dx, int64_t lddx,
+                         float *dgamma, void *workspace, size_t workspace_bytes, void *stream) {
+    return op_rms_backward(M, N, dtype, ptype, dy, lddy, h, ldh, dh, lddh, gamma, rstd, dx, lddx, dgamma, workspace,
+                           workspace_bytes, stream);
+}
+
+int compass_fp8_scale_cols(int K, int *cols) {
+    return op_fp8_scale_cols(K, cols);
+}
+
+int compass_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across, void *x8, void *scale, void
+                      *stream) {
+    return op_fp8_quant(M, K, dtype, x, ldx, across, x8, scale, stream);
+}
+
+int compass_fp8_dequant(int M, int K, int dtype, const void *x8, const void *scale, void *x, int64_t ldx, void
+                        *stream) {
+    return op_fp8_dequant(M, K, dtype, x8, scale, x, ldx, stream);
+}
+
+int compass_fp8_gemm_workspace(int M, int N, int K, size_t *bytes) {
+    return op_fp8_gemm_workspace(M, N, K, bytes);
+}
+
+int compass_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const void *W, const void *W_scale, void
+                     *C, void *workspace, size_t workspace_bytes, void *stream) {
+    return op_fp8_gemm(M, N, K, A, A_scale, W, W_scale, C, workspace, workspace_bytes, stream);
+}
+
+int compass_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes) {
+    return op_fp8_wgrad_workspace(M, N, K, bytes);
+}
+
+int compass_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X8, const void *X_scale, void *dW, int
+                      accumulate, void *workspace, size_t workspace_bytes, void *stream) {
+    return op_fp8_wgrad(M, N, K, gtype, dY, X8, X_scale, dW, accumulate, workspace, workspace_bytes, stream);
+}
+
 int compass_sync(void) { return op_sync(); }
 
 int compass_set_option(int key, long long value) { return op_set_option(key, value); }

@@ -60,4 +60,22 @@ int op_embed_backward(int T, int V, int K, int dtype, int gtype, const int64_t *
                       int64_t ldy, float scale, void *dtable, int64_t ldt, int accumulate, void *workspace, size_t
                       workspace_bytes, void *stream);
 
+// the 8-bit path around the products
+int op_rms_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                   const void *gamma, float eps, void *h, int64_t ldh, void *y, int64_t ldy, void *y8, void *scale,
+                   float *rstd, void *stream);
+int op_rms_workspace(int M, int N, size_t *bytes);
+int op_rms_backward(int M, int N, int dtype, int ptype, const void *dy, int64_t lddy, const void *h, int64_t ldh,
+                    const void *dh, int64_t lddh, const void *gamma, const float *rstd, void *dx, int64_t lddx,
+                    float *dgamma, void *workspace, size_t workspace_bytes, void *stream);
+int op_fp8_scale_cols(int K, int *cols);
+int op_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across, void *x8, void *scale, void *stream);
+int op_fp8_dequant(int M, int K, int dtype, const void *x8, const void *scale, void *x, int64_t ldx, void *stream);
+int op_fp8_gemm_workspace(int M, int N, int K, size_t *bytes);
+int op_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const void *W, const void *W_scale, void *C,
+                void *workspace, size_t workspace_bytes, void *stream);
+int op_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes);
+int op_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X, const void *X_scale, void *dW,
+                 int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
 }  // namespace compass

@@ -1,5 +1,5 @@
-// Device pieces of the row-wise kernels (layer norm, embedding): bf16 and fp32
-// elements by vector, sums over a wave.
+// Device pieces of the row-wise kernels (norms, embedding, 8-bit rows): bf16 and
+// fp32 elements by vector, sums over a wave.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -130,6 +130,38 @@ __device__ __forceinline__ float wave_sum(float x) {
     b = __builtin_bit_cast(uint32_t, x);
     r = __builtin_amdgcn_permlane32_swap(b, b, false, false);
     return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+
+// V parameters of a norm from element i, `none` where there is no such vector.
+template <int V, bool LOOSE>
+__device__ __forceinline__ void load_param(const void *p, int f32, float none, int i, int N, float (&f)[V]) {
+    if (!p) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) f[e] = none;
+    } else if (f32) {
+        unpack(load_pack<float, V, LOOSE>((const float *)p, i, N), f);
+    } else if constexpr (V == 8) {
+        unpack(load_pack<Bf16, V, LOOSE>((const Bf16 *)p, i, N), f);
+    } else {   // half a piece; few enough (once per column) to go by element
+#pragma unroll
+        for (int e = 0; e < V; ++e)
+            f[e] = i + e < N ? __builtin_bit_cast(float, (uint32_t)((const Bf16 *)p)[i + e].bits << 16) : 0.0f;
+    }
+}
+
+// Sum over the TPR threads that share a row, in wave order; `s` holds one
+// value per wave. TPR <= 64: the wave alone, no barrier.
+template <int TPR>
+__device__ __forceinline__ float row_sum(float x, float *s) {
+    x = wave_sum(x);
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = x;
+        __syncthreads();
+        x = s[0];
+#pragma unroll
+        for (int w = 1; w < TPR / 64; ++w) x += s[w];
+    }
+    return x;
 }
 
 }  // namespace compass
