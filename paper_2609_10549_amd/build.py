@@ -28,7 +28,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(HERE, "libcompass.so")
 SAN_LIB = os.path.join(HERE, "libcompass_san.so")
-SOURCES = ["kernels.hip", "noalloc.hip", "xent.hip", "norm.hip", "embed.hip", "rms.hip", "fp8.hip", "fp8_gemm.hip",
+SOURCES = ["kernels.hip", "noalloc.hip", "xent.hip", "norm.hip", "embed.hip", "rms.hip", "fp8.hip", "fp8_gemm.hip", "fp8_wgrad.hip",
            "runtime.cpp", "model.cpp", "abi.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

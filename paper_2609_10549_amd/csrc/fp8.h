@@ -18,6 +18,11 @@ namespace compass {
 constexpr int kGroup = 128;            // values per scale
 constexpr uint32_t kUnitScale = 127;   // the byte of 2^0
 
+// out (bf16 or fp32, `count` values) = the sum of the slices (`stride` floats apart)
+// in order, rounded once; with accumulate, added to what is there.
+hipError_t launch_join_parts(size_t count, size_t stride, int slices, const float *part, void *out, bool f32,
+                             bool accumulate, hipStream_t stream);
+
 // Bytes of the scales of a row of n values: whole words, which the product loads.
 __host__ __device__ constexpr int scale_cols(int n) { return (n + 4 * kGroup - 1) / (4 * kGroup) * 4; }
 

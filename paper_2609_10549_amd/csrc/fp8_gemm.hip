@@ -1,8 +1,6 @@
-// Products of 8-bit rows (fp8.h): an 8-bit product and a weight's gradient from an
-// activation kept in 8 bits.
+// Product of 8-bit rows (fp8.h; compass_fp8_gemm):
 //
-//   compass_fp8_gemm:  C[m][n] = sum_g 2^(sa[m][g] + sw[n][g]) sum_{k in g} A[m][k] W[n][k]
-//   compass_fp8_wgrad: dW[n][k] = sum_m dY[m][n] X[m][k] 2^sx[m][k / 128]
+//   C[m][n] = sum_g 2^(sa[m][g] + sw[n][g]) sum_{k in g} A[m][k] W[n][k]
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -12,8 +10,8 @@
 #include "compass.h"
 #include "fp8.h"
 #include "gemm_core.h"
-#include "internal.h"
 #include "fp8_plan.h"
+#include "internal.h"
 
 namespace compass {
 
@@ -482,92 +480,6 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const ProductP
         if (n + e < p.N) p.C[(size_t)row * (size_t)p.N + n + e] = (uint16_t)pack_bf16x2(x[e], 0.0f);
 }
 
-// The sum of the slices in order, 4 values per thread, rounded once; with
-// accumulate, added to what is there.
-template <bool F32>
-__global__ __launch_bounds__(256) void join_kernel(size_t count, size_t stride, int slices, const float *__restrict__ part,
-                                                   void *out, int accumulate) {
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= count) return;
-    f32x4 x = *reinterpret_cast<const f32x4 *>(part + i);
-#pragma unroll 4
-    for (int s = 1; s < slices; ++s) x += *reinterpret_cast<const f32x4 *>(part + (size_t)s * stride + i);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        if (i + e >= count) break;
-        if constexpr (F32) {
-            float *to = (float *)out + i + e;
-            *to = accumulate ? *to + x[e] : x[e];
-        } else {
-            uint16_t *to = (uint16_t *)out + i + e;
-            *to = (uint16_t)pack_bf16x2(accumulate ? x[e] + __builtin_bit_cast(float, (uint32_t)*to << 16) : x[e], 0.0f);
-        }
-    }
-}
-
-struct GradParams {
-    const uint16_t *dY;
-    const uint8_t *X, *sX;
-    void *dW;
-    int M, N, K, f32, accumulate;
-};
-
-// 64 x 64 tiles of dW, 32 rows of the reduction per stage: both operands turned
-// on their way to LDS, X's values put to bf16 (exactly: four bits and a power of
-// two).
-__global__ __launch_bounds__(256) void grad_kernel(const GradParams p) {
-    __shared__ __attribute__((aligned(16))) uint16_t s[2][64][40];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int n0 = (int)blockIdx.y * 64, k0 = (int)blockIdx.x * 64;
-    const int r = lane & 15, kq = lane >> 4, wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    const int S = scale_cols(p.K);
-    f32x4 acc[2][2];
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    for (int mb = 0; mb < p.M; mb += 32) {
-        __syncthreads();
-        for (int i = 0; i < 8; ++i) {
-            const int at = i * 256 + tid, row = at / 64, col = at % 64, m = mb + row;
-            uint16_t y = 0, x = 0;
-            if (m < p.M && n0 + col < p.N) y = p.dY[(size_t)m * (size_t)p.N + n0 + col];
-            if (m < p.M && k0 + col < p.K) {
-                const int k = k0 + col;
-                const uint32_t byte = p.sX[(size_t)m * S + k / kGroup];
-                float v = ldexpf(__builtin_amdgcn_cvt_f32_fp8((int)p.X[(size_t)m * (size_t)p.K + k], 0), (int)byte - 127);
-                if (byte == 255) v = __builtin_nanf("");
-                x = (uint16_t)pack_bf16x2(v, 0.0f);
-            }
-            s[0][col][row] = y;
-            s[1][col][row] = x;
-        }
-        __syncthreads();
-        bf16x8 a[2], b[2];
-        for (int i = 0; i < 2; ++i) {
-            a[i] = *reinterpret_cast<const bf16x8 *>(&s[0][wm + i * 16 + r][kq * 8]);
-            b[i] = *reinterpret_cast<const bf16x8 *>(&s[1][wn + i * 16 + r][kq * 8]);
-        }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], a[i], acc[i][j], 0, 0, 0);
-    }
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j)
-            for (int e = 0; e < 4; ++e) {
-                const int n = n0 + wm + i * 16 + r, k = k0 + wn + j * 16 + 4 * kq + e;
-                if (n >= p.N || k >= p.K) continue;
-                const size_t at = (size_t)n * (size_t)p.K + k;
-                float x = acc[i][j][e];
-                if (p.f32) {
-                    float *to = (float *)p.dW + at;
-                    *to = p.accumulate ? *to + x : x;
-                } else {
-                    uint16_t *to = (uint16_t *)p.dW + at;
-                    if (p.accumulate) x += __builtin_bit_cast(float, (uint32_t)*to << 16);
-                    *to = (uint16_t)pack_bf16x2(x, 0.0f);
-                }
-            }
-}
-
 template <bool PART>
 hipError_t launch_product(ProductParams p, const TilePlan &pl, hipStream_t stream) {
     const Tile8 &t = kTiles8[pl.cfg];
@@ -599,18 +511,14 @@ hipError_t launch_products(ProductParams p, const TilePlan &pl, float *part, hip
     p.part_stride = part_stride(p.M, p.N);
     hipError_t e = launch_product<true>(p, pl, stream);
     if (e != hipSuccess) return e;
-    const size_t count = (size_t)p.M * (size_t)p.N;
-    join_kernel<false><<<dim3((unsigned)((count + 1023) / 1024)), 256, 0, stream>>>(count, p.part_stride, pl.slices, part,
-                                                                                  p.C, 0);
-    return hipGetLastError();
+    return launch_join_parts((size_t)p.M * (size_t)p.N, p.part_stride, pl.slices, part, p.C, false, false, stream);
 }
 
 constexpr int kMaxRows = 1 << 20, kMaxDepth = 1 << 17;
 
-int check_sizes(int M, int N, int K, bool grad) {
-    if (M < 1 || N < 1 || K < 1 || K % 16 || (grad && N % 8))
-        return set_error(COMPASS_ERR_INVALID, "need positive M, N and K with K a multiple of 16%s",
-                         grad ? ", N of 8" : "");
+int check_sizes(int M, int N, int K) {
+    if (M < 1 || N < 1 || K < 1 || K % 16)
+        return set_error(COMPASS_ERR_INVALID, "need positive M, N and K with K a multiple of 16");
     if (M > kMaxRows || N > kMaxRows || K > kMaxDepth)
         return set_error(COMPASS_ERR_UNSUPPORTED, "M = %d, N = %d, K = %d beyond %d, %d, %d", M, N, K, kMaxRows, kMaxRows,
                          kMaxDepth);
@@ -622,7 +530,7 @@ bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
 }  // namespace
 
 int op_fp8_gemm_workspace(int M, int N, int K, size_t *bytes) {
-    const int rc = check_sizes(M, N, K, false);
+    const int rc = check_sizes(M, N, K);
     if (rc != COMPASS_OK) return rc;
     if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
     *bytes = part_bytes(plan_product(M, N, K), M, N);
@@ -631,7 +539,7 @@ int op_fp8_gemm_workspace(int M, int N, int K, size_t *bytes) {
 
 int op_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const void *W, const void *W_scale, void *C,
                 void *ws, size_t ws_bytes, void *stream) {
-    int rc = check_sizes(M, N, K, false);
+    int rc = check_sizes(M, N, K);
     if (rc != COMPASS_OK) return rc;
     if (!A || !A_scale || !W || !W_scale || !C)
         return set_error(COMPASS_ERR_INVALID, "A, W, their scales and C are required");
@@ -654,34 +562,6 @@ int op_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const v
     p.S = scale_cols(K);
     const hipError_t e = launch_products(p, pl, (float *)ws, (hipStream_t)stream);
     return e == hipSuccess ? COMPASS_OK : set_error(COMPASS_ERR_HIP, "8-bit product launch: %s", hipGetErrorString(e));
-}
-
-int op_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes) {
-    const int rc = check_sizes(M, N, K, true);
-    if (rc != COMPASS_OK) return rc;
-    if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
-    *bytes = 0;
-    return COMPASS_OK;
-}
-
-int op_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X, const void *X_scale, void *dW,
-                 int accumulate, void *ws, size_t ws_bytes, void *stream) {
-    int rc = check_sizes(M, N, K, true);
-    if (rc != COMPASS_OK) return rc;
-    if (gtype != COMPASS_BF16 && gtype != COMPASS_F32)
-        return set_error(COMPASS_ERR_INVALID, "unknown element type %d", gtype);
-    if (accumulate != 0 && accumulate != 1)
-        return set_error(COMPASS_ERR_INVALID, "accumulate = %d, must be 0 or 1", accumulate);
-    if (!dY || !X || !X_scale || !dW) return set_error(COMPASS_ERR_INVALID, "dY, X8, its scale and dW are required");
-    if (misaligned(dY) || misaligned(X) || misaligned(dW) || ((uintptr_t)X_scale & 3))
-        return set_error(COMPASS_ERR_INVALID, "dY, X8 and dW must be 16-byte and the scale 4-byte aligned");
-    int cus;
-    if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
-    const GradParams p{(const uint16_t *)dY, (const uint8_t *)X, (const uint8_t *)X_scale, dW, M, N, K,
-                       gtype == COMPASS_F32, accumulate};
-    grad_kernel<<<dim3((unsigned)((K + 63) / 64), (unsigned)((N + 63) / 64)), 256, 0, (hipStream_t)stream>>>(p);
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? COMPASS_OK : set_error(COMPASS_ERR_HIP, "weight gradient launch: %s", hipGetErrorString(e));
 }
 
 }  // namespace compass

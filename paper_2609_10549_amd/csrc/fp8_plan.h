@@ -60,4 +60,30 @@ inline TilePlan plan_product(int M, int N, int K) {
     return best;
 }
 
+// The weight gradient's tiles (rows of dW, columns) with costs as in kTiles8, a stage
+// being 64 rows of the reduction.
+constexpr int kGradTileCount = 5;
+constexpr Tile8 kGradTiles[kGradTileCount] = {
+    {256, 256, 1, 1.10f, 1.47f, 8.2f}, {256, 128, 1, 0.66f, 0.87f, 4.5f}, {128, 128, 2, 0.44f, 0.93f, 3.1f},
+    {128, 64, 2, 0.35f, 0.60f, 2.1f},  {64, 64, 3, 0.25f, 0.55f, 1.9f},
+};
+inline TilePlan plan_grad(int M, int N, int K) {
+    TilePlan best{};
+    const int stages = (M + 63) / 64;
+    for (int cfg = 0; cfg < kGradTileCount; ++cfg) {
+        const Tile8 &ts = kGradTiles[cfg];
+        const int tn = (N + ts.rows - 1) / ts.rows, tk = (K + ts.cols - 1) / ts.cols;
+        const double slots = (double)kCUs * ts.wg_per_cu;
+        for (int k = 1; k <= kMaxSlices && (k == 1 || (stages / k >= 4 && (double)tn * tk * k <= 2 * slots)); ++k) {
+            const int per = (stages + k - 1) / k, ns = (stages + per - 1) / per;
+            const double rounds = (double)tn * tk * ns / slots, whole = (double)(long)rounds, rest = rounds - whole;
+            double us = 3.0 + whole * (per * ts.full + ts.edge);
+            if (rest > 0) us += per * (ts.alone + (ts.full - ts.alone) * rest * rest) + ts.edge;
+            if (ns > 1) us += 3.0 + (double)N * K * (8.0 * ns + 2.0) / 4.5e6;
+            if (best.tiles_m == 0 || us < best.us) best = {cfg, tn, tk, ns, per * 64, us};
+        }
+    }
+    return best;
+}
+
 }  // namespace compass

@@ -538,6 +538,34 @@ def test_weight_gradient_of_every_code_far_scales_and_nan(M, N, K):
     assert torch.equal(torch.isnan(dw), bad)
 
 
+def test_weight_gradient_under_every_scale():
+    """One row per scale byte, each code under it, one dY of 1 a row: dW is the value
+    itself, in bf16's grid (what is smaller than bf16's normal numbers may be cut to
+    2^-133 steps or to zero on its way)."""
+    torch = _torch()
+    q = torch.arange(256, dtype=torch.uint8, device="cuda").repeat(256, 1)
+    q[:, 127], q[:, 255] = 0x38, 0xB8
+    scale = torch.full((256, 4), 127, dtype=torch.uint8, device="cuda")
+    scale[:, 0] = torch.arange(256, device="cuda")
+    scale[:, 1] = 255 - torch.arange(256, device="cuda")
+    dw = _nan(256, 256)
+    for m0 in range(0, 256, 64):      # 64 rows a call: the others' NaN stays out of the sums
+        rows = slice(m0, m0 + 64)
+        part = _nan(64, 256)
+        C.compass_fp8_wgrad(torch.eye(64, device="cuda").bfloat16(), q[rows].contiguous(), scale[rows].contiguous(), part,
+                            _scratch(C.compass_fp8_wgrad_workspace(64, 64, 256)))
+        dw[rows] = part
+    ref = E.values(q.cpu().numpy(), scale.cpu().numpy())
+    got = _np(dw)
+    # a NaN (byte 255) or an overflow of one row reaches the 64 sums of its columns: 0 times it
+    bad = ~np.isfinite(ref) | (np.abs(ref) > 3.4e38)
+    for m0 in range(0, 256, 64):
+        bad[m0:m0 + 64] |= bad[m0:m0 + 64].any(axis=0)
+    assert not np.isfinite(got[bad]).any() or bad.sum() == 0
+    over = np.abs(got - ref)[~bad] - np.where(np.abs(ref[~bad]) < 2.0 ** -126, 2.0 ** -126, 0.0)
+    assert (over <= 0).all(), over.max()
+
+
 # ------------------------------------------------------------- a run of them
 class Layer:
     """norm -> 8-bit product, and back: what a training step keeps and calls."""
