@@ -18,9 +18,10 @@ namespace compass {
 constexpr int kGroup = 128;            // values per scale
 constexpr uint32_t kUnitScale = 127;   // the byte of 2^0
 
-// out (bf16 or fp32, `count` values) = the sum of the slices (`stride` floats apart)
-// in order, rounded once; with accumulate, added to what is there.
-hipError_t launch_join_parts(size_t count, size_t stride, int slices, const float *part, void *out, bool f32,
+// rows x cols of out (bf16 or fp32, rows ld apart) = the sum of the slices' partial
+// sums (rows of part_ld(cols)) in order, rounded once; with accumulate, added to what is
+// there.
+hipError_t launch_join_parts(int rows, int cols, int slices, const float *part, void *out, int64_t ld, bool f32,
                              bool accumulate, hipStream_t stream);
 
 // Bytes of the scales of a row of n values: whole words, which the product loads.

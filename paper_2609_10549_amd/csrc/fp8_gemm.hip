@@ -22,10 +22,11 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 struct ProductParams {
     const uint8_t *A, *W, *sA, *sW;
     uint16_t *C;
-    float *part;                 // split: fp32 [slices][part_stride], rows of N
-    size_t part_stride;
+    float *part;                 // split: fp32 [slices][part_rows][part_ld], from the first tile on
+    int part_rows, part_ld;
     int M, N, K, S;              // S: bytes of a row of scales
     int tiles_m, tiles_n, group_m;
+    int m_base, n_base;          // the first tile's row and column
     int slices, kslice;          // slices of K (kslice a multiple of 512)
 };
 
@@ -139,8 +140,8 @@ __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductPar
         const int grp = tpos / gsz, rin = tpos - grp * gsz;
         const int rows_here = min(p.group_m, p.tiles_m - grp * p.group_m);
         const int tn = rin / rows_here;
-        t.m0 = (grp * p.group_m + rin - tn * rows_here) * BM;
-        t.n0 = tn * BN;
+        t.m0 = p.m_base + (grp * p.group_m + rin - tn * rows_here) * BM;
+        t.n0 = p.n_base + tn * BN;
         t.kb = t.slice * p.kslice;
         t.ke = min(p.K, t.kb + p.kslice);
         return true;
@@ -341,16 +342,12 @@ __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductPar
                 hold(mi);
                 const int m = m1 + mi * 16 + er;
                 if (m < p.M) {
-                    float *row = p.part + (size_t)cur.slice * p.part_stride + (size_t)m * (size_t)p.N;
+                    float *row = p.part + ((size_t)cur.slice * (size_t)p.part_rows + (size_t)(m - p.m_base)) * (size_t)p.part_ld;
 #pragma unroll
                     for (int ni = 0; ni < FN; ++ni) {
                         const int n = n1 + ni * 16 + 4 * eq;
-                        typedef f32x4 Loose __attribute__((aligned(4)));
-                        if (n + 4 <= p.N) *reinterpret_cast<Loose *>(row + n) = acc[ni][mi];
-                        else
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (n + e < p.N) row[n + e] = acc[ni][mi][e];
+                        // (a row's last vector may end in columns that are not there, and not read)
+                        if (n < p.N) *reinterpret_cast<f32x4 *>(row + n - p.n_base) = acc[ni][mi];
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
@@ -496,22 +493,30 @@ hipError_t launch_product(ProductParams p, const TilePlan &pl, hipStream_t strea
     return hipGetLastError();
 }
 
-hipError_t launch_products(ProductParams p, const TilePlan &pl, float *part, hipStream_t stream) {
-    if (pl.cfg == kFewRows) {
+hipError_t launch_products(ProductParams p, const Cut &cut, float *part, hipStream_t stream) {
+    if (cut.part[0].cfg == kFewRows) {
         few_rows_kernel<<<dim3((unsigned)((p.N + 15) / 16)), kFewWaves * 64, 0, stream>>>(p);
         return hipGetLastError();
     }
-    p.tiles_m = pl.tiles_m;
-    p.tiles_n = pl.tiles_n;
-    p.slices = pl.slices;
-    p.kslice = pl.kslice;
-    p.group_m = kTiles8[pl.cfg].rows == 256 ? 4 : 8;
-    if (pl.slices == 1) return launch_product<false>(p, pl, stream);
-    p.part = part;
-    p.part_stride = part_stride(p.M, p.N);
-    hipError_t e = launch_product<true>(p, pl, stream);
-    if (e != hipSuccess) return e;
-    return launch_join_parts((size_t)p.M * (size_t)p.N, p.part_stride, pl.slices, part, p.C, false, false, stream);
+    for (int i = 0; i < 2 && cut.part[i].tiles_m; ++i) {
+        const TilePlan &pl = cut.part[i];
+        p.tiles_m = pl.tiles_m;
+        p.tiles_n = pl.tiles_n;
+        p.slices = pl.slices;
+        p.kslice = pl.kslice * kGroup;
+        p.group_m = kTiles8[pl.cfg].rows == 256 ? 4 : 8;
+        p.m_base = cut.row0(i);
+        p.n_base = cut.col0(i);
+        p.part = part;
+        p.part_rows = cut.rows_of(i);
+        p.part_ld = part_ld(cut.cols_of(i));
+        hipError_t e = pl.slices > 1 ? launch_product<true>(p, pl, stream) : launch_product<false>(p, pl, stream);
+        if (e == hipSuccess && pl.slices > 1)
+            e = launch_join_parts(cut.rows_of(i), cut.cols_of(i), pl.slices, part,
+                                  p.C + (size_t)p.m_base * (size_t)p.N + p.n_base, p.N, false, false, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 constexpr int kMaxRows = 1 << 20, kMaxDepth = 1 << 17;
@@ -533,7 +538,7 @@ int op_fp8_gemm_workspace(int M, int N, int K, size_t *bytes) {
     const int rc = check_sizes(M, N, K);
     if (rc != COMPASS_OK) return rc;
     if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
-    *bytes = part_bytes(plan_product(M, N, K), M, N);
+    *bytes = plan_product(M, N, K).workspace();
     return COMPASS_OK;
 }
 
@@ -545,8 +550,8 @@ int op_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const v
         return set_error(COMPASS_ERR_INVALID, "A, W, their scales and C are required");
     if (misaligned(A) || misaligned(W) || misaligned(C) || ((uintptr_t)A_scale & 3) || ((uintptr_t)W_scale & 3))
         return set_error(COMPASS_ERR_INVALID, "A, W and C must be 16-byte and the scales 4-byte aligned");
-    const TilePlan pl = plan_product(M, N, K);
-    if (const size_t need = part_bytes(pl, M, N); need && (!ws || misaligned(ws) || ws_bytes < need))
+    const Cut cut = plan_product(M, N, K);
+    if (const size_t need = cut.workspace(); need && (!ws || misaligned(ws) || ws_bytes < need))
         return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes (16-byte aligned), need %zu", ws_bytes, need);
     int cus;
     if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
@@ -560,7 +565,7 @@ int op_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const v
     p.N = N;
     p.K = K;
     p.S = scale_cols(K);
-    const hipError_t e = launch_products(p, pl, (float *)ws, (hipStream_t)stream);
+    const hipError_t e = launch_products(p, cut, (float *)ws, (hipStream_t)stream);
     return e == hipSuccess ? COMPASS_OK : set_error(COMPASS_ERR_HIP, "8-bit product launch: %s", hipGetErrorString(e));
 }
 

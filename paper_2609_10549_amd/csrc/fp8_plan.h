@@ -25,65 +25,106 @@ constexpr Tile8 kTiles8[kTile8Count] = {
 };
 constexpr int kFewMaxRows = 16, kFewMaxDepth = 1 << 15;
 
-// Partial sums of a split product: floats of a slice (whole 16-byte vectors), bytes.
-inline size_t part_stride(int M, int N) { return ((size_t)M * (size_t)N + 3) / 4 * 4; }
-inline size_t part_bytes(const TilePlan &pl, int M, int N) {
-    return pl.slices > 1 ? (size_t)pl.slices * part_stride(M, N) * 4 : 0;
+// Partial sums of a split output (rows x cols of one launch): floats of a row, whole
+// 16-byte vectors, and bytes of all slices.
+__host__ __device__ inline int part_ld(int cols) { return (cols + 3) / 4 * 4; }
+inline size_t part_bytes(int slices, int rows, int cols) {
+    return slices > 1 ? (size_t)slices * (size_t)rows * (size_t)part_ld(cols) * 4 : 0;
 }
 
-// The cheapest tile and, where tiles are fewer than the card's slots, slices of
-// the depth (whole blocks of 512, a word of scales; at least two each); few rows
-// their own kernel, by the weight's way from memory or a workgroup's depth.
-inline TilePlan plan_product(int M, int N, int K) {
+// The cheapest of `count` tiles for a rows x cols output over `stages` stages, and,
+// where tiles are fewer than the card's slots, slices of the reduction: whole units of
+// `unit` stages, at least `least` units each.
+inline TilePlan plan_single(const Tile8 *tiles, int count, int rows, int cols, int stages, int unit, int least) {
     TilePlan best{};
-    const int stages = (K + 127) / 128, blocks = (K + 511) / 512;
-    for (int cfg = 0; cfg < kTile8Count; ++cfg) {
-        const Tile8 &ts = kTiles8[cfg];
-        const int tm = (M + ts.rows - 1) / ts.rows, tn = (N + ts.cols - 1) / ts.cols;
+    const int units = (stages + unit - 1) / unit;
+    for (int cfg = 0; cfg < count; ++cfg) {
+        const Tile8 &ts = tiles[cfg];
+        const int tm = (rows + ts.rows - 1) / ts.rows, tn = (cols + ts.cols - 1) / ts.cols;
         const double slots = (double)kCUs * ts.wg_per_cu;
-        for (int k = 1; k <= kMaxSlices && (k == 1 || (blocks / k >= 2 && (double)tm * tn * k <= 2 * slots)); ++k) {
-            const int per = (blocks + k - 1) / k, ns = (blocks + per - 1) / per;
+        for (int k = 1; k <= kMaxSlices && (k == 1 || (units / k >= least && (double)tm * tn * k <= 2 * slots)); ++k) {
+            const int per = (units + k - 1) / k, ns = (units + per - 1) / per;
             const double rounds = (double)tm * tn * ns / slots, whole = (double)(long)rounds, rest = rounds - whole;
-            const double n = std::min(4 * per, stages);
+            const double n = std::min(unit * per, stages);
             double us = 3.0 + whole * (n * ts.full + ts.edge);
+            // (the power that the busy CUs draw sets the clock of all)
             if (rest > 0) us += n * (ts.alone + (ts.full - ts.alone) * rest * rest) + ts.edge;
             // fp32 slices out and in, and the launch that joins them
-            if (ns > 1) us += 3.0 + (double)M * N * (8.0 * ns + 2.0) / 4.5e6;
-            if (best.tiles_m == 0 || us < best.us) best = {cfg, tm, tn, ns, per * 512, us};
+            if (ns > 1) us += 3.0 + (double)rows * cols * (8.0 * ns + 2.0) / 4.5e6;
+            if (best.tiles_m == 0 || us < best.us) best = {cfg, tm, tn, ns, per * unit, us};
         }
     }
+    return best;
+}
+
+// The same, or two launches along the longer axis: tiles that fill whole rounds of
+// workgroups, then the rest in tiles (and slices) of its own, where the last round of
+// one shape would leave most of the card idle.
+struct Cut {
+    TilePlan part[2];
+    int rows, cols;   // of the output
+    bool along_m;
+    int first;        // length of the long axis in part[0] (the whole of it: one launch)
+    int row0(int i) const { return i && along_m ? first : 0; }
+    int col0(int i) const { return i && !along_m ? first : 0; }
+    int rows_of(int i) const { return !along_m ? rows : i ? rows - first : first; }
+    int cols_of(int i) const { return along_m ? cols : i ? cols - first : first; }
+    size_t workspace() const {   // (one launch's sums are joined before the next one's)
+        size_t most = 0;
+        for (int i = 0; i < 2 && part[i].tiles_m; ++i)
+            most = std::max(most, part_bytes(part[i].slices, rows_of(i), cols_of(i)));
+        return most;
+    }
+};
+inline Cut plan_cut(const Tile8 *tiles, int count, int rows, int cols, int stages, int unit, int least) {
+    const bool along_m = rows >= cols;
+    const int length = along_m ? rows : cols;
+    Cut best{{plan_single(tiles, count, rows, cols, stages, unit, least), {}}, rows, cols, along_m, length};
+    double best_us = best.part[0].us;
+    for (int cfg = 0; cfg < count; ++cfg) {
+        const Tile8 &ts = tiles[cfg];
+        const int tm = (rows + ts.rows - 1) / ts.rows, tn = (cols + ts.cols - 1) / ts.cols;
+        const int across = along_m ? tn : tm, lines_all = along_m ? tm : tn;
+        const long slots = (long)kCUs * ts.wg_per_cu, rounds = (long)tm * tn / slots;
+        for (long r = rounds; r >= 1 && r >= rounds - 1; --r) {
+            const int lines = (int)(r * slots / across), done = lines * (along_m ? ts.rows : ts.cols);
+            const double us = 3.0 + r * ((double)stages * ts.full + ts.edge);
+            if (lines < 1 || lines >= lines_all || us >= best_us) continue;
+            const TilePlan q = along_m ? plan_single(tiles, count, rows - done, cols, stages, unit, least)
+                                       : plan_single(tiles, count, rows, cols - done, stages, unit, least);
+            if (us + q.us < best_us) {
+                best_us = us + q.us;
+                best.part[0] = {cfg, along_m ? lines : tm, along_m ? tn : lines, 1, (stages + unit - 1) / unit * unit, us};
+                best.part[1] = q;
+                best.first = done;
+            }
+        }
+    }
+    return best;
+}
+
+// The 8-bit product: slices are whole blocks of 512 (a word of scales), at least two;
+// few rows have a kernel of their own, bound by the weight's way from memory or by a
+// workgroup's depth.
+inline Cut plan_product(int M, int N, int K) {
+    Cut best = plan_cut(kTiles8, kTile8Count, M, N, (K + 127) / 128, 4, 2);
     if (M <= kFewMaxRows && K <= kFewMaxDepth) {
         const int wgs = (N + 15) / 16, rounds = (wgs + 2 * kCUs - 1) / (2 * kCUs);
         const double us = 3.0 + std::max((double)N * K / 6.5e6, rounds * (1.5 + K * 32.0 / 58e3));
-        if (us < best.us) best = {kFewRows, 1, wgs, 1, K, us};
+        if (us < best.part[0].us + best.part[1].us) best = {{{kFewRows, 1, wgs, 1, (K + 127) / 128, us}, {}}, M, N, true, M};
     }
     return best;
 }
 
-// The weight gradient's tiles (rows of dW, columns) with costs as in kTiles8, a stage
-// being 64 rows of the reduction.
+// The weight gradient's tiles (rows of dW, columns), a stage being 64 rows of the
+// reduction (`alone`: 16 to 256 tiles of 128 stages).
 constexpr int kGradTileCount = 5;
 constexpr Tile8 kGradTiles[kGradTileCount] = {
-    {256, 256, 1, 1.10f, 1.47f, 8.2f}, {256, 128, 1, 0.66f, 0.87f, 4.5f}, {128, 128, 2, 0.44f, 0.93f, 3.1f},
-    {128, 64, 2, 0.35f, 0.60f, 2.1f},  {64, 64, 3, 0.25f, 0.55f, 1.9f},
+    {256, 256, 1, 1.43f, 1.50f, 10.0f}, {256, 128, 1, 0.90f, 0.94f, 6.3f}, {128, 128, 2, 0.64f, 1.04f, 3.9f},
+    {128, 64, 2, 0.56f, 0.80f, 2.3f},   {64, 64, 3, 0.50f, 0.85f, 1.7f},
 };
-inline TilePlan plan_grad(int M, int N, int K) {
-    TilePlan best{};
-    const int stages = (M + 63) / 64;
-    for (int cfg = 0; cfg < kGradTileCount; ++cfg) {
-        const Tile8 &ts = kGradTiles[cfg];
-        const int tn = (N + ts.rows - 1) / ts.rows, tk = (K + ts.cols - 1) / ts.cols;
-        const double slots = (double)kCUs * ts.wg_per_cu;
-        for (int k = 1; k <= kMaxSlices && (k == 1 || (stages / k >= 4 && (double)tn * tk * k <= 2 * slots)); ++k) {
-            const int per = (stages + k - 1) / k, ns = (stages + per - 1) / per;
-            const double rounds = (double)tn * tk * ns / slots, whole = (double)(long)rounds, rest = rounds - whole;
-            double us = 3.0 + whole * (per * ts.full + ts.edge);
-            if (rest > 0) us += per * (ts.alone + (ts.full - ts.alone) * rest * rest) + ts.edge;
-            if (ns > 1) us += 3.0 + (double)N * K * (8.0 * ns + 2.0) / 4.5e6;
-            if (best.tiles_m == 0 || us < best.us) best = {cfg, tn, tk, ns, per * 64, us};
-        }
-    }
-    return best;
+inline Cut plan_grad(int M, int N, int K) {
+    return plan_cut(kGradTiles, kGradTileCount, N, K, (M + 63) / 64, 1, 4);
 }
 
 }  // namespace compass

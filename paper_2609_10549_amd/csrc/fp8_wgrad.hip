@@ -26,11 +26,12 @@ struct GradParams {
     const uint16_t *dY;
     const uint8_t *X, *sX;
     void *dW;
-    float *part;                 // split: fp32 [slices][part_stride], rows of K
-    size_t part_stride;
+    float *part;                 // split: fp32 [slices][part_rows][part_ld], from the first tile on
+    int part_rows, part_ld;
     int M, N, K, S;              // S: bytes of a row of scales
     int f32, accumulate;         // dW in fp32 (else bf16); added to what it holds
     int tiles_n, tiles_k, group_n;
+    int n_base, k_base;          // the first tile's row and column
     int slices, mslice;          // slices of the reduction (mslice a multiple of 64)
 };
 
@@ -48,25 +49,34 @@ __device__ __forceinline__ void each_slot(const Step &step) {
 template <int BK>
 struct XStage {
     static constexpr int J = BK / 64, RB = BK * 2, CPR = BK / 16;   // turns, bytes of an LDS row, chunks of a row
-    u32x4 v[J];
-    uint32_t s[J];
+    static constexpr int STEP = 256 / CPR;                          // rows between a thread's turns
+    static_assert(STEP % 16 == 0, "the same place in the chunks' permutation");
+    struct Piece { u32x4 v[J]; uint32_t s[J]; };
+    uint32_t off[J], soff[J], at[2];
     const uint8_t *x, *sx;      // the next stage's first row, at the tile's first column and group
     int64_t left, sleft;        // bytes to the operands' ends
-    __device__ __forceinline__ void init(const GradParams &p, int k0, int mb) {
+    __device__ __forceinline__ void init(const GradParams &p, int k0, int mb, int tid) {
         const uint64_t o = (uint64_t)mb * (uint64_t)p.K + (uint64_t)k0;
         const uint64_t so = (uint64_t)mb * (uint64_t)p.S + (uint64_t)(k0 / kGroup);
         x = p.X + o;
         sx = p.sX + so;
         left = (int64_t)((uint64_t)p.M * (uint64_t)p.K) - (int64_t)o;
         sleft = (int64_t)((uint64_t)p.M * (uint64_t)p.S) - (int64_t)so;
+        const int row = tid / CPR, c = tid % CPR;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            off[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.K + (uint32_t)c * 16u;
+            soff[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.S + (uint32_t)(c * 16 / kGroup);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) at[h] = (uint32_t)(row * RB + (((2 * c + h) ^ cross_swizzle<RB>(row)) << 4));
     }
     // Rows behind the last are zeros under the smallest scale, whatever dY's rows there are.
-    __device__ __forceinline__ void load(const GradParams &p, int j, int tid) {
+    __device__ __forceinline__ void load(Piece &t, int j) const {
         const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void *)x, (short)0, bound(left), 0x00020000);
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)sx, (short)0, bound(sleft), 0x00020000);
-        const int row = (j * 256 + tid) / CPR, c = (j * 256 + tid) % CPR;
-        v[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, row * p.K + c * 16, 0, 0);
-        s[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, row * p.S + c * 16 / kGroup, 0, 0);
+        t.v[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)off[j], 0, 0);
+        t.s[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)soff[j], 0, 0);
     }
     __device__ __forceinline__ static int bound(int64_t n) {
         return (int)(n < 0 ? 0 : n < (int64_t)kTileSpanMax ? n : (int64_t)kTileSpanMax);
@@ -78,26 +88,35 @@ struct XStage {
         sleft -= (int64_t)64 * p.S;
     }
     // half h (8 values) of turn j to the stage at LDS offset buf
-    __device__ __forceinline__ void put(int j, int h, uint32_t buf, int tid) const {
-        const int row = (j * 256 + tid) / CPR, c = 2 * ((j * 256 + tid) % CPR) + h;
+    __device__ __forceinline__ void put(const Piece &t, int j, int h, uint32_t buf) const {
         // (the conversion takes the scale's exponent field, which is the byte; 255 is NaN there too)
-        const float scale = __builtin_bit_cast(float, s[j] << 23 | (s[j] == 255u ? 1u << 22 : 0u));
+        const float scale = __builtin_bit_cast(float, t.s[j] << 23 | (t.s[j] == 255u ? 1u << 22 : 0u));
         u32x4 o;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t w = v[j][2 * h + e];
+            const uint32_t w = t.v[j][2 * h + e];
             o[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
             o[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
         }
         typedef __attribute__((address_space(3))) u32x4 lds16;
-        *(lds16 *)(uintptr_t)(buf + (uint32_t)(row * RB + ((c ^ cross_swizzle<RB>(row)) << 4))) = o;
+        ((lds16 *)(uintptr_t)(buf + at[h]))[j * STEP * RB / 16] = o;
     }
-    // the registers hold a whole stage from here on: the compiler waits here
-    __device__ __forceinline__ void arrived() {
+    // t holds a whole stage from here on: the compiler waits here
+    __device__ __forceinline__ static void arrived(Piece &t) {
 #pragma unroll
-        for (int j = 0; j < J; ++j) asm volatile("" : "+v"(v[j]), "+v"(s[j]));
+        for (int j = 0; j < J; ++j) asm volatile("" : "+v"(t.v[j]), "+v"(t.s[j]));
     }
 };
+
+// Block f of substep S of the stage at LDS offset buf, as Reader<true>::read.
+template <int S, int RB, class R>
+__device__ __forceinline__ bf16x8 fragment(const R &r, uint32_t buf, int f) {
+    typedef __attribute__((address_space(3))) s16x4 lds4;
+    lds4 *q = (lds4 *)(uintptr_t)(buf + r.at[f]) + S * 4 * RB;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(q + RB / 2);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
 
 // BN x BK tiles of dW, 4 waves, 2 x 2 over the tile, two stage buffers (64 of the
 // reduction) of each operand, one barrier per stage.
@@ -129,8 +148,8 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
         const int grp = tpos / gsz, rin = tpos - grp * gsz;
         const int rows_here = min(p.group_n, p.tiles_n - grp * p.group_n);
         const int tk = rin / rows_here;
-        t.n0 = (grp * p.group_n + rin - tk * rows_here) * BN;
-        t.k0 = tk * BK;
+        t.n0 = p.n_base + (grp * p.group_n + rin - tk * rows_here) * BN;
+        t.k0 = p.k_base + tk * BK;
         t.mb = t.slice * p.mslice;
         t.me = min(p.M, t.mb + p.mslice);
         return true;
@@ -145,10 +164,11 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
     auto load_dy = [&](int j, i32x4 r, uint32_t buf) __attribute__((always_inline)) {
         dma16(r, ld.off[j], buf + (uint32_t)((j * 4 + wave) * 1024));
     };
-    auto begin = [&](const Tile &t) {   // the first two stages, and the third's X in registers
+    typename XStage<BK>::Piece x0, x1;
+    auto begin = [&](const Tile &t) {   // the loads of the first two stages
         const int id = fresh(tid);
         ld.init(p.dY, (uint64_t)p.M * (uint64_t)p.N * 2u, t.n0, p.N, p.N, t.mb, t.me, id & 63, wave);
-        xs.init(p, t.k0, t.mb);
+        xs.init(p, t.k0, t.mb, id);
         i32x4 r;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -156,14 +176,12 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
             asm volatile("s_nop 4" : "+s"(r));
 #pragma unroll
             for (int j = 0; j < LD; ++j) load_dy(j, r, lds0 + i * SD);
-#pragma unroll
-            for (int j = 0; j < xs.J; ++j) xs.load(p, j, id);
-            xs.next(p);
-#pragma unroll
-            for (int h = 0; h < 2 * xs.J; ++h) xs.put(h / 2, h % 2, ldsX + i * SX, id);
         }
 #pragma unroll
-        for (int j = 0; j < xs.J; ++j) xs.load(p, j, id);
+        for (int j = 0; j < xs.J; ++j) xs.load(x0, j);
+        xs.next(p);
+#pragma unroll
+        for (int j = 0; j < xs.J; ++j) xs.load(x1, j);
         xs.next(p);
     };
 
@@ -187,17 +205,24 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
         {
             Reader<true, BN, FN> ra;
             Reader<true, BK, FK> rb;
-            const int id = fresh(tid), l = id & 63;
+            const int l = fresh(lane);
             ra.init(wn0, l);
             rb.init(wk0, l);
             const int MT = (cur.me - cur.mb + kBK - 1) / kBK;
+#pragma unroll
+            for (int h = 0; h < 2 * xs.J; ++h) xs.put(x0, h / 2, h % 2, ldsX);
+#pragma unroll
+            for (int h = 0; h < 2 * xs.J; ++h) xs.put(x1, h / 2, h % 2, ldsX + SX);
+#pragma unroll
+            for (int j = 0; j < xs.J; ++j) xs.load(x0, j);   // the third stage's
+            xs.next(p);
             __builtin_amdgcn_s_waitcnt(0);
             lds_barrier();
             bf16x8 a0[FN], b0[FK], a1[FN], b1[FK];
 #pragma unroll
-            for (int f = 0; f < FN; ++f) a0[f] = ra.template read<0>(lds0, f);
+            for (int f = 0; f < FN; ++f) a0[f] = fragment<0, 2 * BN>(ra, lds0, f);
 #pragma unroll
-            for (int f = 0; f < FK; ++f) b0[f] = rb.template read<0>(ldsX, f);
+            for (int f = 0; f < FK; ++f) b0[f] = fragment<0, 2 * BK>(rb, ldsX, f);
             uint32_t dC = lds0, xC = ldsX;
             i32x4 r;
             pin();
@@ -212,8 +237,8 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
 #pragma unroll
                     for (int f = 0; f < FN + FK; ++f)
                         if (slot_of(f, FN + FK, 0, RE) == I) {
-                            if (f >= 1 && f <= FN) a1[f - 1] = ra.template read<1>(dC, f - 1);
-                            else b1[f == 0 ? 0 : f - FN] = rb.template read<1>(xC, f == 0 ? 0 : f - FN);
+                            if (f >= 1 && f <= FN) a1[f - 1] = fragment<1, 2 * BN>(ra, dC, f - 1);
+                            else b1[f == 0 ? 0 : f - FN] = fragment<1, 2 * BK>(rb, xC, f == 0 ? 0 : f - FN);
                         }
                     __builtin_amdgcn_sched_barrier(0);
                 });
@@ -224,15 +249,15 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
 #pragma unroll
                         for (int f = 0; f < FN + FK; ++f)
                             if (slot_of(f, FN + FK, B1, NM) == I) {
-                                if (f >= 1 && f <= FN) a0[f - 1] = ra.template read<0>(dN, f - 1);
-                                else b0[f == 0 ? 0 : f - FN] = rb.template read<0>(xN, f == 0 ? 0 : f - FN);
+                                if (f >= 1 && f <= FN) a0[f - 1] = fragment<0, 2 * BN>(ra, dN, f - 1);
+                                else b0[f == 0 ? 0 : f - FN] = fragment<0, 2 * BK>(rb, xN, f == 0 ? 0 : f - FN);
                             }
                         constexpr int XE = B1 + (NM - B1) / 2, DE = B1 + (NM - B1) * 3 / 4;
 #pragma unroll
                         for (int h = 0; h < 2 * xs.J; ++h)
                             if (slot_of(h, 2 * xs.J, B1, XE) == I) {
-                                xs.put(h / 2, h % 2, xC, id);
-                                if (h % 2 == 1) xs.load(p, h / 2, id);
+                                xs.put(x0, h / 2, h % 2, xC);
+                                if (h % 2 == 1) xs.load(x0, h / 2);
                             }
 #pragma unroll
                         for (int j = 0; j < LD; ++j)
@@ -247,7 +272,7 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
                 // take the stage after it
                 wait_vm_lgkm0<0>();
                 lds_barrier();
-                xs.arrived();
+                xs.arrived(x0);
                 each_slot<B1, NM>(second);
                 xs.next(p);
                 dC = dN;
@@ -281,32 +306,35 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
             for (int it = 0; it < NIT; ++it) {
                 const int row = (it * 64 + et) / CPR, j = (it * 64 + et) % CPR;
                 const char *w = region + row * RB;
-                f32x4 x0 = *reinterpret_cast<const f32x4 *>(w + (((2 * j) ^ (row & 7)) << 4));
-                f32x4 x1 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + 1) ^ (row & 7)) << 4));
+                f32x4 y0 = *reinterpret_cast<const f32x4 *>(w + (((2 * j) ^ (row & 7)) << 4));
+                f32x4 y1 = *reinterpret_cast<const f32x4 *>(w + (((2 * j + 1) ^ (row & 7)) << 4));
                 const int n = n1 + ni * 16 + row, k = k1 + j * 8;
                 if (n >= p.N || k >= p.K) continue;   // K is a multiple of 16
                 const size_t at = (size_t)n * (size_t)p.K + k;
                 if (p.part || p.f32) {
-                    float *to = p.part ? p.part + (size_t)cur.slice * p.part_stride + at : (float *)p.dW + at;
+                    float *to = (float *)p.dW + at;
+                    if (p.part)
+                        to = p.part + ((size_t)cur.slice * (size_t)p.part_rows + (size_t)(n - p.n_base)) * (size_t)p.part_ld +
+                             (k - p.k_base);
                     if (!p.part && p.accumulate) {
-                        x0 += *reinterpret_cast<const f32x4 *>(to);
-                        x1 += *reinterpret_cast<const f32x4 *>(to + 4);
+                        y0 += *reinterpret_cast<const f32x4 *>(to);
+                        y1 += *reinterpret_cast<const f32x4 *>(to + 4);
                     }
-                    *reinterpret_cast<f32x4 *>(to) = x0;
-                    *reinterpret_cast<f32x4 *>(to + 4) = x1;
+                    *reinterpret_cast<f32x4 *>(to) = y0;
+                    *reinterpret_cast<f32x4 *>(to + 4) = y1;
                 } else {
                     u32x4 *to = reinterpret_cast<u32x4 *>((uint16_t *)p.dW + at);
                     if (p.accumulate) {
                         const u32x4 was = *to;
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            f32x4 &x = e < 2 ? x0 : x1;
+                            f32x4 &x = e < 2 ? y0 : y1;
                             x[2 * (e & 1)] += __builtin_bit_cast(float, was[e] << 16);
                             x[2 * (e & 1) + 1] += __builtin_bit_cast(float, was[e] & 0xFFFF0000u);
                         }
                     }
-                    *to = u32x4{pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]),
-                                pack_bf16x2(x1[2], x1[3])};
+                    *to = u32x4{pack_bf16x2(y0[0], y0[1]), pack_bf16x2(y0[2], y0[3]), pack_bf16x2(y1[0], y1[1]),
+                                pack_bf16x2(y1[2], y1[3])};
                 }
             }
             asm volatile("" ::: "memory");
@@ -319,47 +347,62 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
 // The sum of the slices in order, 4 values per thread, rounded once; with
 // accumulate, added to what is there.
 template <bool F32>
-__global__ __launch_bounds__(256) void join_kernel(size_t count, size_t stride, int slices, const float *__restrict__ part,
-                                                   void *out, int accumulate) {
-    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+__global__ __launch_bounds__(256) void join_kernel(int rows, int cols, int slices, const float *__restrict__ part, void *out,
+                                                   int64_t ld, int accumulate) {
+    const uint32_t per = (uint32_t)part_ld(cols) / 4, count = (uint32_t)rows * per;
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i >= count) return;
-    f32x4 x = *reinterpret_cast<const f32x4 *>(part + i);
+    const f32x4 *from = reinterpret_cast<const f32x4 *>(part) + i;
+    f32x4 x = *from;
 #pragma unroll 4
-    for (int s = 1; s < slices; ++s) x += *reinterpret_cast<const f32x4 *>(part + (size_t)s * stride + i);
+    for (int s = 1; s < slices; ++s) x += from[(size_t)s * count];
+    const uint32_t row = i / per, c = (i - row * per) * 4;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        if (i + e >= count) break;
+        if ((int)c + e >= cols) break;
+        const int64_t at = (int64_t)row * ld + c + e;
         if constexpr (F32) {
-            float *to = (float *)out + i + e;
+            float *to = (float *)out + at;
             *to = accumulate ? *to + x[e] : x[e];
         } else {
-            uint16_t *to = (uint16_t *)out + i + e;
+            uint16_t *to = (uint16_t *)out + at;
             *to = (uint16_t)pack_bf16x2(accumulate ? x[e] + __builtin_bit_cast(float, (uint32_t)*to << 16) : x[e], 0.0f);
         }
     }
 }
 
-hipError_t launch_grad(GradParams p, const TilePlan &pl, float *part, hipStream_t stream) {
-    p.tiles_n = pl.tiles_m;
-    p.tiles_k = pl.tiles_n;
-    p.slices = pl.slices;
-    p.mslice = pl.kslice;
-    p.group_n = kGradTiles[pl.cfg].rows == 256 ? 4 : 8;
-    p.part_stride = part_stride(p.N, p.K);
-    p.part = pl.slices > 1 ? part : nullptr;
-    const int64_t items = (int64_t)pl.tiles_m * pl.tiles_n * pl.slices;
-    const dim3 grid((unsigned)std::min<int64_t>(items, kCUs * kGradTiles[pl.cfg].wg_per_cu));
-    switch (pl.cfg) {   // (a template instance for each row of kGradTiles)
-    case 0: grad_kernel<256, 256, 1><<<grid, kThreads, 0, stream>>>(p); break;
-    case 1: grad_kernel<256, 128, 1><<<grid, kThreads, 0, stream>>>(p); break;
-    case 2: grad_kernel<128, 128, 2><<<grid, kThreads, 0, stream>>>(p); break;
-    case 3: grad_kernel<128, 64, 2><<<grid, kThreads, 0, stream>>>(p); break;
-    default: grad_kernel<64, 64, 3><<<grid, kThreads, 0, stream>>>(p); break;
+hipError_t launch_grad(GradParams p, const Cut &cut, float *part, hipStream_t stream) {
+    for (int i = 0; i < 2 && cut.part[i].tiles_m; ++i) {
+        const TilePlan &pl = cut.part[i];
+        p.tiles_n = pl.tiles_m;
+        p.tiles_k = pl.tiles_n;
+        p.slices = pl.slices;
+        p.mslice = pl.kslice * kBK;
+        p.group_n = kGradTiles[pl.cfg].rows == 256 ? 4 : 8;
+        p.n_base = cut.row0(i);
+        p.k_base = cut.col0(i);
+        p.part = pl.slices > 1 ? part : nullptr;
+        p.part_rows = cut.rows_of(i);
+        p.part_ld = part_ld(cut.cols_of(i));
+        const int64_t items = (int64_t)pl.tiles_m * pl.tiles_n * pl.slices;
+        const dim3 grid((unsigned)std::min<int64_t>(items, kCUs * kGradTiles[pl.cfg].wg_per_cu));
+        switch (pl.cfg) {   // (a template instance for each row of kGradTiles)
+        case 0: grad_kernel<256, 256, 1><<<grid, kThreads, 0, stream>>>(p); break;
+        case 1: grad_kernel<256, 128, 1><<<grid, kThreads, 0, stream>>>(p); break;
+        case 2: grad_kernel<128, 128, 2><<<grid, kThreads, 0, stream>>>(p); break;
+        case 3: grad_kernel<128, 64, 2><<<grid, kThreads, 0, stream>>>(p); break;
+        default: grad_kernel<64, 64, 3><<<grid, kThreads, 0, stream>>>(p); break;
+        }
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess && pl.slices > 1) {
+            const size_t at = (size_t)p.n_base * (size_t)p.K + (size_t)p.k_base;
+            void *to = p.f32 ? (void *)((float *)p.dW + at) : (void *)((uint16_t *)p.dW + at);
+            e = launch_join_parts(cut.rows_of(i), cut.cols_of(i), pl.slices, part, to, p.K, p.f32 != 0, p.accumulate != 0,
+                                  stream);
+        }
+        if (e != hipSuccess) return e;
     }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || pl.slices == 1) return e;
-    return launch_join_parts((size_t)p.N * (size_t)p.K, p.part_stride, pl.slices, part, p.dW, p.f32 != 0, p.accumulate != 0,
-                             stream);
+    return hipSuccess;
 }
 
 constexpr int kMaxRows = 1 << 20, kMaxDepth = 1 << 17;
@@ -377,11 +420,12 @@ bool misaligned(const void *p) { return ((uintptr_t)p & 15) != 0; }
 
 }  // namespace
 
-hipError_t launch_join_parts(size_t count, size_t stride, int slices, const float *part, void *out, bool f32,
+hipError_t launch_join_parts(int rows, int cols, int slices, const float *part, void *out, int64_t ld, bool f32,
                              bool accumulate, hipStream_t stream) {
-    const dim3 grid((unsigned)((count + 1023) / 1024));
-    if (f32) join_kernel<true><<<grid, 256, 0, stream>>>(count, stride, slices, part, out, accumulate);
-    else join_kernel<false><<<grid, 256, 0, stream>>>(count, stride, slices, part, out, accumulate);
+    // (a split output has at most 1024 tiles: below 2^32 threads)
+    const dim3 grid((unsigned)(((size_t)rows * (size_t)(part_ld(cols) / 4) + 255) / 256));
+    if (f32) join_kernel<true><<<grid, 256, 0, stream>>>(rows, cols, slices, part, out, ld, accumulate);
+    else join_kernel<false><<<grid, 256, 0, stream>>>(rows, cols, slices, part, out, ld, accumulate);
     return hipGetLastError();
 }
 
@@ -389,7 +433,7 @@ int op_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes) {
     const int rc = check_sizes(M, N, K);
     if (rc != COMPASS_OK) return rc;
     if (!bytes) return set_error(COMPASS_ERR_INVALID, "bytes is required");
-    *bytes = part_bytes(plan_grad(M, N, K), N, K);
+    *bytes = plan_grad(M, N, K).workspace();
     return COMPASS_OK;
 }
 
@@ -404,8 +448,8 @@ int op_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X, 
     if (!dY || !X || !X_scale || !dW) return set_error(COMPASS_ERR_INVALID, "dY, X8, its scale and dW are required");
     if (misaligned(dY) || misaligned(X) || misaligned(dW) || ((uintptr_t)X_scale & 3))
         return set_error(COMPASS_ERR_INVALID, "dY, X8 and dW must be 16-byte and the scale 4-byte aligned");
-    const TilePlan pl = plan_grad(M, N, K);
-    if (const size_t need = part_bytes(pl, N, K); need && (!ws || misaligned(ws) || ws_bytes < need))
+    const Cut cut = plan_grad(M, N, K);
+    if (const size_t need = cut.workspace(); need && (!ws || misaligned(ws) || ws_bytes < need))
         return set_error(COMPASS_ERR_INVALID, "workspace of %zu bytes (16-byte aligned), need %zu", ws_bytes, need);
     int cus;
     if ((rc = current_num_cu(&cus)) != COMPASS_OK) return rc;
@@ -420,7 +464,7 @@ int op_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X, 
     p.S = scale_cols(K);
     p.f32 = gtype == COMPASS_F32;
     p.accumulate = accumulate;
-    const hipError_t e = launch_grad(p, pl, (float *)ws, (hipStream_t)stream);
+    const hipError_t e = launch_grad(p, cut, (float *)ws, (hipStream_t)stream);
     return e == hipSuccess ? COMPASS_OK : set_error(COMPASS_ERR_HIP, "weight gradient launch: %s", hipGetErrorString(e));
 }
 
