@@ -120,8 +120,8 @@ inline Cut plan_product(int M, int N, int K) {
 // reduction (`alone`: 16 to 256 tiles of 128 stages).
 constexpr int kGradTileCount = 5;
 constexpr Tile8 kGradTiles[kGradTileCount] = {
-    {256, 256, 1, 1.43f, 1.50f, 10.0f}, {256, 128, 1, 0.90f, 0.94f, 6.3f}, {128, 128, 2, 0.64f, 1.04f, 3.9f},
-    {128, 64, 2, 0.56f, 0.80f, 2.3f},   {64, 64, 3, 0.50f, 0.85f, 1.7f},
+    {256, 256, 1, 1.43f, 1.50f, 9.5f}, {256, 128, 1, 0.90f, 0.94f, 5.3f}, {128, 128, 2, 0.64f, 1.04f, 3.9f},
+    {128, 64, 2, 0.56f, 0.80f, 2.6f},  {64, 64, 3, 0.50f, 0.85f, 2.3f},
 };
 inline Cut plan_grad(int M, int N, int K) {
     return plan_cut(kGradTiles, kGradTileCount, N, K, (M + 63) / 64, 1, 4);

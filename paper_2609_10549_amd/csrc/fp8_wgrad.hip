@@ -320,8 +320,13 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
                         y0 += *reinterpret_cast<const f32x4 *>(to);
                         y1 += *reinterpret_cast<const f32x4 *>(to + 4);
                     }
-                    *reinterpret_cast<f32x4 *>(to) = y0;
-                    *reinterpret_cast<f32x4 *>(to + 4) = y1;
+                    if (p.part) {
+                        *reinterpret_cast<f32x4 *>(to) = y0;
+                        *reinterpret_cast<f32x4 *>(to + 4) = y1;
+                    } else {
+                        __builtin_nontemporal_store(y0, reinterpret_cast<f32x4 *>(to));
+                        __builtin_nontemporal_store(y1, reinterpret_cast<f32x4 *>(to + 4));
+                    }
                 } else {
                     u32x4 *to = reinterpret_cast<u32x4 *>((uint16_t *)p.dW + at);
                     if (p.accumulate) {
@@ -333,8 +338,9 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
                             x[2 * (e & 1) + 1] += __builtin_bit_cast(float, was[e] & 0xFFFF0000u);
                         }
                     }
-                    *to = u32x4{pack_bf16x2(y0[0], y0[1]), pack_bf16x2(y0[2], y0[3]), pack_bf16x2(y1[0], y1[1]),
-                                pack_bf16x2(y1[2], y1[3])};
+                    const u32x4 o = {pack_bf16x2(y0[0], y0[1]), pack_bf16x2(y0[2], y0[3]), pack_bf16x2(y1[0], y1[1]),
+                                     pack_bf16x2(y1[2], y1[3])};
+                    __builtin_nontemporal_store(o, to);
                 }
             }
             asm volatile("" ::: "memory");
