@@ -1,13 +1,36 @@
 """What the entry points of the MLP in 8 bits refuse before they enqueue anything,
 and the sizes they give (no GPU)."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 
 from paper_2609_10549_amd import compass as C
 
+HERE = os.path.dirname(os.path.abspath(__file__))
+CSRC = os.path.join(os.path.dirname(HERE), "paper_2609_10549_amd", "csrc")
 P = 4096     # an aligned address
 BIG = 1 << 40
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="needs a host C++ compiler")
+def test_plans_cover_their_outputs_and_the_gpu_tests_reach_every_launch(tmp_path):
+    from tests import test_gpu_eight_bits as small
+    from tests import test_gpu_eight_bits_plans as plans
+    exe = tmp_path / "fp8_plan_check"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", f"-I{CSRC}", "-o", str(exe),
+                    os.path.join(HERE, "fp8_plan_check.cpp")], check=True)
+    sizes = [f"0,{M},{N},{K}" for M, N, K in small.PRODUCT + plans.PRODUCT]
+    sizes += [f"1,{M},{N},{K}" for M, N, K in small.GRAD + plans.GRAD]
+    out = subprocess.run([str(exe)] + sizes, capture_output=True, text=True, timeout=120)
+    assert out.returncode == 0, out.stdout + out.stderr
+    lines = out.stdout.split("\n")
+    assert lines[0].startswith("ok ") and int(lines[0].split()[1]) > 8000
+    reached = {ln for ln in lines[1:] if ln and not ln.startswith("any ")}
+    used = {ln[4:] for ln in lines if ln.startswith("any ")}
+    assert used - reached == set()
 
 
 def test_scale_columns_are_whole_words():
