@@ -391,22 +391,25 @@ __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductPar
     }
 }
 
-// Few rows (at most 16): a workgroup takes 16 columns, each of its waves every
+// Few rows (at most 16 MT): a workgroup takes 16 columns, each of its waves every
 // kFewWaves-th block of 512 of the depth (a word of scales per row). A wave streams
 // its own stages of A and W through a ring of kFewRing buffers of its own in LDS, so
 // no barrier joins the waves before their sums are added in wave order. (Straight to
 // registers in the matrix core's layout, where neighbouring lanes hold different
 // rows, a load takes a clock per lane: 8 x 6144 x 12288 21.9 us, a CU 33 bytes per ns.)
 constexpr int kFewWaves = 8, kFewRing = 2, kFewDepth = kFewMaxDepth;
+template <int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const ProductParams p) {
-    constexpr int SB = 4096;   // 16 rows of A, then of W, 128 bytes each
-    constexpr int L = 4;       // loads per stage
+    constexpr int SB = (MT + 1) * 2048;   // A's rows, then W's, 128 bytes each
+    constexpr int L = 2 * MT + 2;         // loads per stage
+    constexpr int ROWS = 16 * MT + 16;
     constexpr int RING = kFewWaves * kFewRing * SB;
-    __shared__ __attribute__((aligned(1024))) char smem[RING + 32 * (kFewDepth / kGroup)];
+    __shared__ __attribute__((aligned(1024))) char smem[RING + ROWS * (kFewDepth / kGroup)];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n0 = (int)blockIdx.x * 16;
-    RowLoader<16, 1> la, lw;
+    RowLoader<16 * MT, 1> la;
+    RowLoader<16, 1> lw;
     la.init(p.A, 0, p.M, p.K, lane, 0);
     lw.init(p.W, n0, p.N, p.K, lane, 0);
     const uint32_t ring = (uint32_t)(uintptr_t)LDS_AS(smem) + (uint32_t)(wave * kFewRing * SB);
@@ -420,57 +423,63 @@ __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const ProductP
             lw.cut(k0, p.K, lane, 0);
         }
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            lw.load(q, k0, buf + 2048, 0);
-            la.load(q, k0, buf, 0);
-        }
+        for (int q = 0; q < 2; ++q) lw.load(q, k0, buf + MT * 2048, 0);
+#pragma unroll
+        for (int q = 0; q < 2 * MT; ++q) la.load(q, k0, buf, 0);
     };
 #pragma unroll
     for (int i = 0; i < kFewRing; ++i) load_stage(i);
-    // the scales of the 32 rows, words of four stages
+    // the rows' scales, words of four stages
     const int words = p.S / 4;
     int *const scales = reinterpret_cast<int *>(smem + RING);
-    for (int at = tid; at < 32 * words; at += kFewWaves * 64) {
+    for (int at = tid; at < ROWS * words; at += kFewWaves * 64) {
         const int row = at / words, word = at % words;
-        const uint8_t *from = row < 16 ? p.sA + (size_t)min(row, p.M - 1) * (size_t)p.S
-                                       : p.sW + (size_t)min(n0 + row - 16, p.N - 1) * (size_t)p.S;
+        const uint8_t *from = row < 16 * MT ? p.sA + (size_t)min(row, p.M - 1) * (size_t)p.S
+                                       : p.sW + (size_t)min(n0 + row - 16 * MT, p.N - 1) * (size_t)p.S;
         scales[at] = *reinterpret_cast<const int *>(from + 4 * word);
     }
     __syncthreads();
-    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    f32x4 acc[MT];
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) acc[mt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int r = lane & 15, kq = lane >> 4, swz = (r >> 1) & 7;
     const char *const frag = smem + wave * kFewRing * SB + r * 128;
-    int sa = 0, sw = 0;
+    int sa[MT] = {}, sw = 0;
     for (int i = 0; place(i) < p.K; ++i) {
         if ((i & 3) == 0) {
             const int word = wave + kFewWaves * (i >> 2);
-            sa = scales[r * words + word];
-            sw = scales[(16 + r) * words + word];
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) sa[mt] = scales[(mt * 16 + r) * words + word];
+            sw = scales[(MT * 16 + r) * words + word];
         }
         wait_vm_lgkm0<(kFewRing - 1) * L>();
         const char *f = frag + (i % kFewRing) * SB;
-        i32x4 h[4];
+        i32x8 v[MT + 1];   // A's blocks, then W's
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            h[q] = *reinterpret_cast<const i32x4 *>(f + (q & 2) * 1024 + (((4 * (q & 1) + kq) ^ swz) << 4));
+        for (int q = 0; q <= MT; ++q) {
+            const i32x4 lo = *reinterpret_cast<const i32x4 *>(f + q * 2048 + ((kq ^ swz) << 4));
+            const i32x4 hi = *reinterpret_cast<const i32x4 *>(f + q * 2048 + (((4 + kq) ^ swz) << 4));
+            v[q] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the stage is in registers before its buffer is refilled
         load_stage(i + kFewRing);
         const int sh = 8 * (i & 3);
-        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
-            __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3, 4, 5, 6, 7),
-            __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7), acc, 0, 0, 0, (int)((uint32_t)sw >> sh), 0,
-            (int)((uint32_t)sa >> sh));
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt)
+            acc[mt] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v[MT], v[mt], acc[mt], 0, 0, 0, (int)((uint32_t)sw >> sh),
+                                                                       0, (int)((uint32_t)sa[mt] >> sh));
     }
     wait_vm_lgkm0<0>();   // the loads issued past the end have landed
     __syncthreads();
     f32x4 *sum = reinterpret_cast<f32x4 *>(smem);   // partial sums [wave][row][16 columns]
-    sum[(wave * 16 + r) * 4 + kq] = acc;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) sum[((wave * MT + mt) * 16 + r) * 4 + kq] = acc[mt];
     __syncthreads();
-    if (tid >= 64) return;
+    if (tid >= MT * 64) return;
     const int row = tid >> 2, n = n0 + (tid & 3) * 4;
     f32x4 x = sum[tid];
 #pragma unroll
-    for (int q = 1; q < kFewWaves; ++q) x += sum[q * 64 + tid];
+    for (int q = 1; q < kFewWaves; ++q) x += sum[q * MT * 64 + tid];
     if (row >= p.M) return;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -495,7 +504,10 @@ hipError_t launch_product(ProductParams p, const TilePlan &pl, hipStream_t strea
 
 hipError_t launch_products(ProductParams p, const Cut &cut, float *part, hipStream_t stream) {
     if (cut.part[0].cfg == kFewRows) {
-        few_rows_kernel<<<dim3((unsigned)((p.N + 15) / 16)), kFewWaves * 64, 0, stream>>>(p);
+        const dim3 grid((unsigned)((p.N + 15) / 16));
+        if (p.M <= 16) few_rows_kernel<1><<<grid, kFewWaves * 64, 0, stream>>>(p);
+        else if (p.M <= 32) few_rows_kernel<2><<<grid, kFewWaves * 64, 0, stream>>>(p);
+        else few_rows_kernel<3><<<grid, kFewWaves * 64, 0, stream>>>(p);
         return hipGetLastError();
     }
     for (int i = 0; i < 2 && cut.part[i].tiles_m; ++i) {

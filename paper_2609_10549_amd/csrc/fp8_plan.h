@@ -23,7 +23,7 @@ constexpr Tile8 kTiles8[kTile8Count] = {
     {256, 256, 1, 1.10f, 1.33f, 8.0f}, {256, 128, 1, 0.66f, 0.80f, 5.8f}, {128, 128, 2, 0.50f, 0.88f, 3.7f},
     {128, 128, 1, 0.44f, 0.52f, 3.0f}, {128, 64, 2, 0.47f, 0.62f, 2.4f},  {64, 64, 2, 0.30f, 0.43f, 1.8f},
 };
-constexpr int kFewMaxRows = 16, kFewMaxDepth = 1 << 15;
+constexpr int kFewMaxRows = 48, kFewMaxDepth = 1 << 15;
 
 // Partial sums of a split output (rows x cols of one launch): floats of a row, whole
 // 16-byte vectors, and bytes of all slices.
@@ -104,13 +104,17 @@ inline Cut plan_cut(const Tile8 *tiles, int count, int rows, int cols, int stage
 }
 
 // The 8-bit product: slices are whole blocks of 512 (a word of scales), at least two;
-// few rows have a kernel of their own, bound by the weight's way from memory or by a
-// workgroup's depth.
+// few rows have a kernel of their own, bound by the weight's way from memory, by all
+// operands' way from the caches (A once per 16 columns), or by a workgroup's depth (two
+// on a CU with up to 16 rows, else one). 48 x 4096 x 4096 7.6 us, in slices of tiles
+// 10.1; 32 x 6144 x 12288 20.6, in slices 18.6.
 inline Cut plan_product(int M, int N, int K) {
     Cut best = plan_cut(kTiles8, kTile8Count, M, N, (K + 127) / 128, 4, 2);
     if (M <= kFewMaxRows && K <= kFewMaxDepth) {
-        const int wgs = (N + 15) / 16, rounds = (wgs + 2 * kCUs - 1) / (2 * kCUs);
-        const double us = 3.0 + std::max((double)N * K / 6.5e6, rounds * (1.5 + K * 32.0 / 58e3));
+        const int blocks = (M + 15) / 16, wgs = (N + 15) / 16, slots = blocks == 1 ? 2 * kCUs : kCUs;
+        const int rounds = (wgs + slots - 1) / slots;
+        const double way = K * 16.0 * (blocks + 1);   // bytes of a workgroup
+        const double us = 3.0 + std::max({(double)N * K / 5.6e6, wgs * way / 13e6, rounds * (1.5 + way / 80e3)});
         if (us < best.part[0].us + best.part[1].us) best = {{{kFewRows, 1, wgs, 1, (K + 127) / 128, us}, {}}, M, N, true, M};
     }
     return best;

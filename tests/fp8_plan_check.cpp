@@ -21,7 +21,7 @@ static bool check(int op, int M, int N, int K, Reached &r) {
     const int stages = op ? (M + 63) / 64 : (K + 127) / 128, unit = op ? 1 : 4;
     if (c.rows != rows || c.cols != cols) return false;
     if (c.part[0].cfg == kFewRows && !op) {
-        r.insert({op, kFewRows, 0, 0});
+        r.insert({op, kFewRows, 0, (M - 1) / 16});   // (the blocks of rows in the place of the part)
         return M <= kFewMaxRows && K <= kFewMaxDepth && c.workspace() == 0 && c.part[1].tiles_m == 0;
     }
     const int length = c.along_m ? rows : cols;
@@ -49,7 +49,7 @@ int main(int argc, char **argv) {
     Reached any, given;
     long sizes = 0;
     for (int op : {0, 1})
-        for (int M : {1, 2, 8, 16, 17, 64, 65, 130, 300, 520, 777, 913, 1100, 2100, 3000, 3760, 4096, 5555, 8192, 16384, 70000, 1 << 20})
+        for (int M : {1, 2, 8, 16, 17, 33, 48, 64, 65, 130, 300, 520, 777, 913, 1100, 2100, 3000, 3760, 4096, 5555, 8192, 16384, 70000, 1 << 20})
             for (int N : {8, 64, 72, 136, 600, 1160, 1536, 2600, 4096, 5003, 6144, 9352, 12000, 13170, 16384, 54001, 1 << 20})
                 for (int K : {16, 144, 528, 1040, 1552, 2048, 3008, 4208, 6144, 8208, 12288, 16384, 32784, 131072}) {
                     if (!check(op, M, op ? N / 8 * 8 : N, K, any)) return std::printf("op %d M %d N %d K %d\n", op, M, N, K), 1;

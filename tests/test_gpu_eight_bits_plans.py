@@ -20,7 +20,7 @@ PRODUCT = [(643, 12241, 272), (386, 16325, 3568), (257, 10963, 128), (130, 13419
            (5935, 2755, 3344), (3341, 2321, 3616), (4384, 1901, 2960), (16, 5003, 32768), (16, 77, 32784), (5, 40, 131072),
            (300, 300, 131056), (5400, 385, 22560), (2751, 3862, 32960), (12478, 1825, 3728), (656, 3515, 12208),
            (1950, 5055, 20352), (5097, 1876, 10752), (1813, 10232, 784), (3357, 2632, 7296), (19771, 1164, 144),
-           (1686, 5044, 7248)]
+           (1686, 5044, 7248), (17, 4096, 4096), (32, 515, 8208), (33, 2048, 1552), (48, 4096, 4096), (47, 100, 32768)]
 GRAD = [(129, 3744, 4304), (917, 928, 8144), (1, 528, 6560), (1, 392, 7136), (1, 64, 128), (7723, 664, 5520),
         (8141, 136, 4080), (2506, 136, 4624), (1982, 72, 2592), (720, 64, 128), (259, 2112, 7744), (1319, 4560, 5376),
         (760, 3728, 4368), (1010, 2256, 3616), (924, 1328, 6000), (197, 8296, 1728), (969, 5280, 1424), (1, 2328, 1712),
