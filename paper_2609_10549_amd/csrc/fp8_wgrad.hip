@@ -53,48 +53,50 @@ struct XStage {
     static_assert(STEP % 16 == 0, "the same place in the chunks' permutation");
     struct Piece { u32x4 v[J]; uint32_t s[J]; };
     uint32_t off[J], soff[J], at[2];
+    bool odd;                   // the lane's halves go out in the other order
     const uint8_t *x, *sx;      // the next stage's first row, at the tile's first column and group
-    int64_t left, sleft;        // bytes to the operands' ends
+    int left;                   // rows from there to the last
     __device__ __forceinline__ void init(const GradParams &p, int k0, int mb, int tid) {
-        const uint64_t o = (uint64_t)mb * (uint64_t)p.K + (uint64_t)k0;
-        const uint64_t so = (uint64_t)mb * (uint64_t)p.S + (uint64_t)(k0 / kGroup);
-        x = p.X + o;
-        sx = p.sX + so;
-        left = (int64_t)((uint64_t)p.M * (uint64_t)p.K) - (int64_t)o;
-        sleft = (int64_t)((uint64_t)p.M * (uint64_t)p.S) - (int64_t)so;
+        x = p.X + (uint64_t)mb * (uint64_t)p.K + (uint64_t)k0;
+        sx = p.sX + (uint64_t)mb * (uint64_t)p.S + (uint64_t)(k0 / kGroup);
+        left = p.M - mb;
         const int row = tid / CPR, c = tid % CPR;
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             off[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.K + (uint32_t)c * 16u;
             soff[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.S + (uint32_t)(c * 16 / kGroup);
         }
+        // 8 neighbouring lanes' first halves lie in every other chunk: the next 8
+        // lanes write their second ones with them, so that 16 lanes meet all banks
+        odd = (tid >> 3) & 1;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) at[h] = (uint32_t)(row * RB + (((2 * c + h) ^ cross_swizzle<RB>(row)) << 4));
+        for (int h = 0; h < 2; ++h) at[h] = (uint32_t)(row * RB + (((2 * c + (odd ? 1 - h : h)) ^ cross_swizzle<RB>(row)) << 4));
     }
     // Rows behind the last are zeros under the smallest scale, whatever dY's rows there are.
-    __device__ __forceinline__ void load(Piece &t, int j) const {
-        const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void *)x, (short)0, bound(left), 0x00020000);
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void *)sx, (short)0, bound(sleft), 0x00020000);
+    __device__ __forceinline__ void load(const GradParams &p, int k0, Piece &t, int j) const {
+        const int rows = min(left, 128);   // (a stage reads 64, of its last one past the row's end)
+        const __amdgpu_buffer_rsrc_t rx =
+            __builtin_amdgcn_make_buffer_rsrc((void *)x, (short)0, max(rows * p.K - k0, 0), 0x00020000);
+        const __amdgpu_buffer_rsrc_t rs =
+            __builtin_amdgcn_make_buffer_rsrc((void *)sx, (short)0, max(rows * p.S - k0 / kGroup, 0), 0x00020000);
         t.v[j] = __builtin_amdgcn_raw_buffer_load_b128(rx, (int)off[j], 0, 0);
         t.s[j] = __builtin_amdgcn_raw_buffer_load_b8(rs, (int)soff[j], 0, 0);
-    }
-    __device__ __forceinline__ static int bound(int64_t n) {
-        return (int)(n < 0 ? 0 : n < (int64_t)kTileSpanMax ? n : (int64_t)kTileSpanMax);
     }
     __device__ __forceinline__ void next(const GradParams &p) {
         x += (int64_t)64 * p.K;
         sx += (int64_t)64 * p.S;
-        left -= (int64_t)64 * p.K;
-        sleft -= (int64_t)64 * p.S;
+        left -= 64;
     }
-    // half h (8 values) of turn j to the stage at LDS offset buf
+    // half h (8 values; of the lanes that are odd the other one) of turn j to the stage
+    // at LDS offset buf
     __device__ __forceinline__ void put(const Piece &t, int j, int h, uint32_t buf) const {
         // (the conversion takes the scale's exponent field, which is the byte; 255 is NaN there too)
         const float scale = __builtin_bit_cast(float, t.s[j] << 23 | (t.s[j] == 255u ? 1u << 22 : 0u));
         u32x4 o;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            const uint32_t w = t.v[j][2 * h + e];
+            const uint32_t mine = t.v[j][2 * h + e], other = t.v[j][2 - 2 * h + e];
+            const uint32_t w = odd ? other : mine;
             o[2 * e] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
             o[2 * e + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true));
         }
@@ -178,10 +180,10 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
             for (int j = 0; j < LD; ++j) load_dy(j, r, lds0 + i * SD);
         }
 #pragma unroll
-        for (int j = 0; j < xs.J; ++j) xs.load(x0, j);
+        for (int j = 0; j < xs.J; ++j) xs.load(p, t.k0, x0, j);
         xs.next(p);
 #pragma unroll
-        for (int j = 0; j < xs.J; ++j) xs.load(x1, j);
+        for (int j = 0; j < xs.J; ++j) xs.load(p, t.k0, x1, j);
         xs.next(p);
     };
 
@@ -214,7 +216,7 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
 #pragma unroll
             for (int h = 0; h < 2 * xs.J; ++h) xs.put(x1, h / 2, h % 2, ldsX + SX);
 #pragma unroll
-            for (int j = 0; j < xs.J; ++j) xs.load(x0, j);   // the third stage's
+            for (int j = 0; j < xs.J; ++j) xs.load(p, cur.k0, x0, j);   // the third stage's
             xs.next(p);
             __builtin_amdgcn_s_waitcnt(0);
             lds_barrier();
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p)
                         for (int h = 0; h < 2 * xs.J; ++h)
                             if (slot_of(h, 2 * xs.J, B1, XE) == I) {
                                 xs.put(x0, h / 2, h % 2, xC);
-                                if (h % 2 == 1) xs.load(x0, h / 2);
+                                if (h % 2 == 1) xs.load(p, cur.k0, x0, h / 2);
                             }
 #pragma unroll
                         for (int j = 0; j < LD; ++j)
