@@ -66,9 +66,10 @@ struct XStage {
             off[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.K + (uint32_t)c * 16u;
             soff[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.S + (uint32_t)(c * 16 / kGroup);
         }
-        // 8 neighbouring lanes' first halves lie in every other chunk: the next 8
-        // lanes write their second ones with them, so that 16 lanes meet all banks
-        odd = (tid >> 3) & 1;
+        // 4 neighbouring lanes' first halves lie in every other chunk: the next 4 lanes
+        // write their second ones with them, so that the 8 lanes that LDS takes at a
+        // time meet all banks
+        odd = (tid >> 2) & 1;
 #pragma unroll
         for (int h = 0; h < 2; ++h) at[h] = (uint32_t)(row * RB + (((2 * c + (odd ? 1 - h : h)) ^ cross_swizzle<RB>(row)) << 4));
     }
