@@ -451,7 +451,8 @@ int compass_rms_backward(int M, int N, int dtype, int ptype, const void *dy, int
  * the products of 8 consecutive k to the largest of the 8 and cuts them at 2^-13 of
  * its binade, far below the values' own 2^-4; nothing else is lost before fp32.) With dY and the
  * transposed weight in 8-bit rows it is the gradient of the activation. K a
- * multiple of 16 up to 2^17, M and N up to 2^20. */
+ * multiple of 16 up to 2^17, M and N up to 2^20. The workspace holds partial sums of
+ * outputs with few tiles; NULL where compass_fp8_gemm_workspace gives 0. */
 int compass_fp8_gemm_workspace(int M, int N, int K, size_t *bytes);
 int compass_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, const void *W, const void *W_scale,
                      void *C, void *workspace, size_t workspace_bytes, void *stream);
@@ -461,7 +462,7 @@ int compass_fp8_gemm(int M, int N, int K, const void *A, const void *A_scale, co
  * x8): dY M x N bf16, dW N x K of type gtype, packed and 16-byte aligned. The values
  * enter the matrix cores in bf16 (exact down to 2^-126), products accumulate in fp32.
  * accumulate = 1 adds to dW what it holds before the one rounding. N a multiple of 8,
- * K of 16; M and N up to 2^20, K up to 2^17. */
+ * K of 16; M and N up to 2^20, K up to 2^17. The workspace as compass_fp8_gemm's. */
 int compass_fp8_wgrad_workspace(int M, int N, int K, size_t *bytes);
 int compass_fp8_wgrad(int M, int N, int K, int gtype, const void *dY, const void *X8, const void *X_scale, void *dW,
                       int accumulate, void *workspace, size_t workspace_bytes, void *stream);

@@ -95,9 +95,26 @@ __device__ __forceinline__ void each_slot(const Step &step) {
     }
 }
 
-// BM x BN tiles, 4 waves, 2 x 2 over the tile, NB stage buffers of A and W, a
+// BM x BN tiles, 4 waves, WC of them along the columns, NB stage buffers of A and W, a
 // group of 128 per stage: one scaled MFMA per block of 16 x 16 and stage, which
-// multiplies by both scales itself.
+// multiplies by both scales itself (a lane's chunks kq and kq + 4 of a row's group lie
+// the same way in both operands, and all lanes of a row hold its one scale). Workgroups
+// stay and take a tile of every round; the next tile's first stages load under the
+// epilogue.
+//
+// What bounds it: the large tiles, the matrix cores at the clock that the power
+// allows. 8192 x 6144 x 12288 449 to 459 us from card to card (2.70 to 2.76 PFLOP/s; MFMA
+// busy 0.68 at 1.87 GHz; the library's product with one scale for all, 455 us on N(0, 1)
+// and 400 on these values). On the way there: a barrier per stage, loads in its last
+// column of blocks and its scales by bytes 514 us; two barriers, the loads over half of
+// the stage 478; columns in pairs, scales by words of four stages, their addresses in
+// vector registers 466; a stage's place as the loads' scalar offset 459. What did not
+// help: waiting for no load at all (so latency is not it), touching lines a stage
+// earlier (600), other groups of row tiles (2: 504, 8: 485), 192 x 256 tiles (575).
+//
+// Small products are bound by a tile's edges and, between one and two workgroups per
+// CU, by the CUs that have two: 777 x 5003 x 1552 16 us (280 tiles), 768 x 5120 x 1536 11
+// (240).
 template <int BM, int BN, int WC, int NB, int WGS, bool PART>
 __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductParams p) {
     constexpr int WM = BM * WC / 4, WN = BN / WC, FM = WM / 16, FN = WN / 16, NM = FM * FN;
@@ -245,8 +262,8 @@ __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductPar
             uint32_t bA = lds0, bW = ldsW, sc = 0u;   // this stage's buffers, the word of its scales
             // Every accumulator in a register of its own, here and at each call: without
             // it the compiler rotates them from the constant zero on, and moves a part's
-            // MFMAs behind the barrier and the branch that follow it, where they are used
-            // next (19 of the first 20 of a stage: 8192 x 6144 x 12288 478 us).
+            // MFMAs behind the barrier and the branch that follow it, where their results
+            // are used next (19 of a stage's first 20).
             auto pin = [&]() __attribute__((always_inline)) {
 #pragma unroll
                 for (int i = 0; i < NM; ++i) {
@@ -394,9 +411,11 @@ __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductPar
 // Few rows (at most 16 MT): a workgroup takes 16 columns, each of its waves every
 // kFewWaves-th block of 512 of the depth (a word of scales per row). A wave streams
 // its own stages of A and W through a ring of kFewRing buffers of its own in LDS, so
-// no barrier joins the waves before their sums are added in wave order. (Straight to
-// registers in the matrix core's layout, where neighbouring lanes hold different
-// rows, a load takes a clock per lane: 8 x 6144 x 12288 21.9 us, a CU 33 bytes per ns.)
+// no barrier joins the waves before their sums are added in wave order.
+//
+// Bound by memory: 8 x 6144 x 12288 14.1 us (75 MB of W at 5.3 TB/s), with 1 to 16 rows.
+// (Straight to registers in the matrix core's layout, where neighbouring lanes hold
+// different rows, a load takes a clock per lane: 21.9 us, and 26.3 with 16 rows.)
 constexpr int kFewWaves = 8, kFewRing = 2, kFewDepth = kFewMaxDepth;
 template <int MT>
 __global__ __launch_bounds__(kFewWaves * 64) void few_rows_kernel(const ProductParams p) {

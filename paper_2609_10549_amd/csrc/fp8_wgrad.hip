@@ -122,7 +122,20 @@ __device__ __forceinline__ bf16x8 fragment(const R &r, uint32_t buf, int f) {
 }
 
 // BN x BK tiles of dW, 4 waves, 2 x 2 over the tile, two stage buffers (64 of the
-// reduction) of each operand, one barrier per stage.
+// reduction) of each operand, one barrier per stage: behind it the stage is in
+// registers, and its buffers take dY's stage after the next one by loads that go to
+// LDS, X's from the registers where it has been on its way for a stage.
+//
+// What bounds it: the large tiles, the transposed reads and the matrix cores at the
+// clock that the power allows, 1.25 to 1.35 PFLOP/s in whole rounds (8192 x 4096 x 4096
+// 203 to 219 us from card to card), and what X costs beside them, 0.2 of the time
+// (without its conversion and loads 0.8; a conversion is a slow operation). 8192 x 6144 x
+// 12288 973 to 1010 us: 4.5 rounds of 256 x 256 tiles, three of them and three of 256 x
+// 128. Few rows: dW's stores, 64 x 6144 x 12288 45 us (3.4 TB/s). Between them latency: 777
+// x 5000 x 1552 26 to 30 us, two rounds of 13 stages. What did not help: conversions over
+// three quarters of a stage in place of a half, the barrier later, three or four
+// workgroups of the small tiles per CU in place of two and three (26.9 -> 28.8), 64 x 128
+// tiles for 128 x 64 (31), 192 x 256 tiles (1011).
 template <int BN, int BK, int WGS>
 __global__ __launch_bounds__(kThreads, WGS) void grad_kernel(const GradParams p) {
     constexpr int FN = BN / 32, FK = BK / 32, NM = FN * FK;   // blocks of 16 x 16 of a wave
