@@ -109,8 +109,8 @@ __device__ __forceinline__ void each_slot(const Step &step) {
 // column of blocks and its scales by bytes 514 us; two barriers, the loads over half of
 // the stage 478; columns in pairs, scales by words of four stages, their addresses in
 // vector registers 466; a stage's place as the loads' scalar offset 459. What did not
-// help: waiting for no load at all (so latency is not it), touching lines a stage
-// earlier (600), other groups of row tiles (2: 504, 8: 485), 192 x 256 tiles (575).
+// help, beside 484 to 489: touching lines a stage earlier (596 to 601), groups of 2 row
+// tiles in place of 4 (504 to 507) or of 8 (480 to 490), 192 x 256 tiles (575).
 //
 // Small products are bound by a tile's edges and, between one and two workgroups per
 // CU, by the CUs that have two: 777 x 5003 x 1552 16 us (280 tiles), 768 x 5120 x 1536 11
