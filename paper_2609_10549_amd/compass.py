@@ -640,6 +640,28 @@ def _eight(x, scale, what: str, shape: tuple, k: _Kinds) -> tuple:
             _typed(scale, f"{what}'s scale", (shape[0], 4 * -(-shape[1] // 512)), k.scale))
 
 
+_current_device = _stream_of = None
+
+
+def _find_current_device():
+    """A function giving the number of the current device (and, where this torch
+    has it, one giving the address of a device's current stream)."""
+    import torch
+    global _current_device, _stream_of
+    _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device
+
+
+def _stream_by(x, stream) -> int | None:
+    """As _stream, for operands that lie beside x: on the current GPU, where a launch
+    goes, else ValueError. (One operand is asked, and the current device once.)"""
+    here, at = (_current_device or _find_current_device())(), x.get_device()
+    if at != here:
+        raise ValueError(f"operands on GPU {at}, the current one is {here}")
+    return _stream_of(at) if stream is None and _stream_of else _stream(stream)
+
+
 def _sizes(name: str, *sizes) -> int:
     out = ctypes.c_size_t()
     _check(getattr(lib(), name)(*sizes, ctypes.byref(out)), name)
@@ -653,7 +675,7 @@ def compass_fp8_quant(x, x8, scale, across: bool = False, stream=None) -> None:
     shape = M, K = _dims(x, "x")
     rc = (_lib or lib()).compass_fp8_quant(
         M, K, _kind(x), *_rows(x, "x", shape, k.elements), 1 if across else 0,
-        *_eight(x8, scale, "x8", (K, M) if across else (M, K), k), _stream(stream))
+        *_eight(x8, scale, "x8", (K, M) if across else (M, K), k), _stream_by(x, stream))
     if rc < 0:
         _check(rc, "compass_fp8_quant")
 
@@ -665,7 +687,7 @@ def compass_fp8_dequant(x8, scale, x, stream=None) -> None:
     shape = M, K = _dims(x, "x")
     at, ld = _rows(x, "x", shape, k.elements)
     rc = (_lib or lib()).compass_fp8_dequant(M, K, _kind(x), *_eight(x8, scale, "x8", shape, k), at, ld,
-                                             _stream(stream))
+                                             _stream_by(x, stream))
     if rc < 0:
         _check(rc, "compass_fp8_dequant")
 
@@ -684,7 +706,7 @@ def compass_rms_forward(x, gamma, y, rstd, residual=None, h=None, y8=None, scale
         *(none if residual is None else _rows(residual, "residual", shape, kind)), g, eps,
         *(none if h is None else _rows(h, "h", shape, kind)), *(none if y is None else _rows(y, "y", shape, kind)),
         *(none if y8 is None and scale is None else _eight(y8, scale, "y8", shape, k)),
-        _typed(rstd, "rstd", (M,), k.float), _stream(stream))
+        _typed(rstd, "rstd", (M,), k.float), _stream_by(x, stream))
     if rc < 0:
         _check(rc, "compass_rms_forward")
 
@@ -705,7 +727,7 @@ def compass_rms_backward(dy, h, gamma, rstd, dx, dgamma, workspace, dh=None, str
         M, N, _kind(h), ptype, *_rows(dy, "dy", shape, kind), *_rows(h, "h", shape, k.elements),
         *((None, 0) if dh is None else _rows(dh, "dh", shape, kind)), g, _typed(rstd, "rstd", (M,), k.float),
         *_rows(dx, "dx", shape, kind), _typed(dgamma, "dgamma", (N,), k.float),
-        *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+        *((None, 0) if workspace is None else _ws(workspace)), _stream_by(h, stream))
     if rc < 0:
         _check(rc, "compass_rms_backward")
 
@@ -722,7 +744,7 @@ def compass_fp8_gemm(A, A_scale, W, W_scale, C, workspace, stream=None) -> None:
     N = _dims(W, "W")[0]
     rc = (_lib or lib()).compass_fp8_gemm(
         M, N, K, *_eight(A, A_scale, "A", shape, k), *_eight(W, W_scale, "W", (N, K), k),
-        _typed(C, "C", (M, N), k.bits), *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+        _typed(C, "C", (M, N), k.bits), *((None, 0) if workspace is None else _ws(workspace)), _stream_by(A, stream))
     if rc < 0:
         _check(rc, "compass_fp8_gemm")
 
@@ -742,7 +764,7 @@ def compass_fp8_wgrad(dY, X8, X_scale, dW, workspace, accumulate: bool = False, 
     rc = (_lib or lib()).compass_fp8_wgrad(
         M, N, K, _kind(dW), _typed(dY, "dY", (M, N), k.bits), *_eight(X8, X_scale, "X8", (M, K), k),
         _typed(dW, "dW", (N, K), k.elements), 1 if accumulate else 0,
-        *((None, 0) if workspace is None else _ws(workspace)), _stream(stream))
+        *((None, 0) if workspace is None else _ws(workspace)), _stream_by(dY, stream))
     if rc < 0:
         _check(rc, "compass_fp8_wgrad")
 

@@ -216,3 +216,28 @@ def test_operands_whose_sizes_are_read_are_tensors():
             for other in (None, P):
                 with pytest.raises(ValueError, match="must be a tensor"):
                     f(**{**o[f], n: other}, stream=0)
+
+
+def test_operands_on_another_gpu_are_refused(monkeypatch):
+    class Away(OnGpu):
+        def get_device(self):
+            return 1
+    monkeypatch.setattr(C, "_current_device", lambda: 0)
+    for f, operands in _calls().items():
+        away = {n: Away(*x.shape, dtype=x.dtype) for n, x in operands.items()}
+        with pytest.raises(ValueError, match="on GPU 1, the current one is 0"):
+            f(**away, stream=0)
+
+
+def test_the_current_gpu_is_found_at_the_first_call(monkeypatch):
+    import torch
+    monkeypatch.setattr(C, "_current_device", None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 3, raising=False)
+
+    class Here(OnGpu):
+        def get_device(self):
+            return 3
+    for _ in range(2):
+        assert C._stream_by(Here(2, 2), 7) == 7
+        with pytest.raises(ValueError, match="the current one is 3"):
+            C._stream_by(OnGpu(2, 2), 7)

@@ -685,3 +685,20 @@ def test_layers_on_two_streams_at_once():
     for L, w in zip(layers, want):
         for k, v in L.outputs().items():
             assert torch.equal(v, w[k]), k
+
+
+def test_operands_on_another_gpu_than_the_current_one_are_refused(monkeypatch):
+    """(The current one is said to be another: nothing is enqueued.)"""
+    torch = _torch()
+    L = Layer(5, 16, 32, seed=3)
+    L.step()
+    torch.cuda.synchronize()
+    want = L.outputs()
+    here = torch.cuda.current_device()
+    monkeypatch.setattr(C, "_current_device", lambda: here + 1)
+    with pytest.raises(ValueError, match=f"on GPU {here}, the current one is {here + 1}"):
+        L.step()
+    monkeypatch.undo()
+    torch.cuda.synchronize()
+    for k, v in L.outputs().items():
+        assert torch.equal(v, want[k]), k
