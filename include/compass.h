@@ -400,9 +400,9 @@ int compass_embed_backward(int T, int V, int K, int dtype, int gtype, const int6
  * The norm before the products, the products, and what the backward pass reads
  * of them. Same conventions as the operators above: device pointers, caller-owned
  * workspaces, no allocation, no state, any stream, graph capture, the same bits
- * on every call. Operands and stream are the current device's (the Python binding
- * refuses others). Sizes are at least 1; no operand may overlap another except where
- * it is said.
+ * on every call. Operands, workspace and stream are the current device's (the Python
+ * binding refuses tensors and streams of others). Sizes are at least 1; no operand may
+ * overlap another except where it is said.
  *
  * 8-bit rows: R rows of n values are R x n bytes of e4m3 (1 sign, 4 exponent, 3
  * fraction bits, largest 448, no infinity), 16-byte aligned, and R x S bytes of

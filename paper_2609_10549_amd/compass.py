@@ -653,13 +653,23 @@ def _find_current_device():
     return _current_device
 
 
-def _stream_by(x, stream) -> int | None:
-    """As _stream, for operands that lie beside x: on the current GPU, where a launch
-    goes, else ValueError. (One operand is asked, and the current device once.)"""
-    here, at = (_current_device or _find_current_device())(), x.get_device()
+def _stream_by(x, stream, *others) -> int | None:
+    """As _stream, for operands x and others that lie on the current GPU, where a
+    launch goes, and a stream of that GPU, else ValueError. (The current GPU is asked
+    once. Operands that are None or plain addresses, and a stream that is one, have no
+    GPU to ask.)"""
+    here = (_current_device or _find_current_device())()
+    for o in (x, *others):
+        if o is not None and not isinstance(o, int) and o.get_device() != here:
+            raise ValueError(f"operands on GPU {o.get_device()}, the current one is {here}")
+    if stream is None:
+        return _stream_of(here) if _stream_of else _stream(None)
+    if isinstance(stream, int):
+        return stream
+    at = getattr(stream, "device_index", here)
     if at != here:
-        raise ValueError(f"operands on GPU {at}, the current one is {here}")
-    return _stream_of(at) if stream is None and _stream_of else _stream(stream)
+        raise ValueError(f"stream on GPU {at}, the current one is {here}")
+    return stream.cuda_stream
 
 
 def _sizes(name: str, *sizes) -> int:
@@ -675,7 +685,7 @@ def compass_fp8_quant(x, x8, scale, across: bool = False, stream=None) -> None:
     shape = M, K = _dims(x, "x")
     rc = (_lib or lib()).compass_fp8_quant(
         M, K, _kind(x), *_rows(x, "x", shape, k.elements), 1 if across else 0,
-        *_eight(x8, scale, "x8", (K, M) if across else (M, K), k), _stream_by(x, stream))
+        *_eight(x8, scale, "x8", (K, M) if across else (M, K), k), _stream_by(x, stream, x8, scale))
     if rc < 0:
         _check(rc, "compass_fp8_quant")
 
@@ -687,7 +697,7 @@ def compass_fp8_dequant(x8, scale, x, stream=None) -> None:
     shape = M, K = _dims(x, "x")
     at, ld = _rows(x, "x", shape, k.elements)
     rc = (_lib or lib()).compass_fp8_dequant(M, K, _kind(x), *_eight(x8, scale, "x8", shape, k), at, ld,
-                                             _stream_by(x, stream))
+                                             _stream_by(x, stream, x8, scale))
     if rc < 0:
         _check(rc, "compass_fp8_dequant")
 
@@ -706,7 +716,7 @@ def compass_rms_forward(x, gamma, y, rstd, residual=None, h=None, y8=None, scale
         *(none if residual is None else _rows(residual, "residual", shape, kind)), g, eps,
         *(none if h is None else _rows(h, "h", shape, kind)), *(none if y is None else _rows(y, "y", shape, kind)),
         *(none if y8 is None and scale is None else _eight(y8, scale, "y8", shape, k)),
-        _typed(rstd, "rstd", (M,), k.float), _stream_by(x, stream))
+        _typed(rstd, "rstd", (M,), k.float), _stream_by(x, stream, residual, gamma, h, y, y8, scale, rstd))
     if rc < 0:
         _check(rc, "compass_rms_forward")
 
@@ -727,7 +737,8 @@ def compass_rms_backward(dy, h, gamma, rstd, dx, dgamma, workspace, dh=None, str
         M, N, _kind(h), ptype, *_rows(dy, "dy", shape, kind), *_rows(h, "h", shape, k.elements),
         *((None, 0) if dh is None else _rows(dh, "dh", shape, kind)), g, _typed(rstd, "rstd", (M,), k.float),
         *_rows(dx, "dx", shape, kind), _typed(dgamma, "dgamma", (N,), k.float),
-        *((None, 0) if workspace is None else _ws(workspace)), _stream_by(h, stream))
+        *((None, 0) if workspace is None else _ws(workspace)),
+        _stream_by(h, stream, dy, dh, gamma, rstd, dx, dgamma, workspace))
     if rc < 0:
         _check(rc, "compass_rms_backward")
 
@@ -744,7 +755,8 @@ def compass_fp8_gemm(A, A_scale, W, W_scale, C, workspace, stream=None) -> None:
     N = _dims(W, "W")[0]
     rc = (_lib or lib()).compass_fp8_gemm(
         M, N, K, *_eight(A, A_scale, "A", shape, k), *_eight(W, W_scale, "W", (N, K), k),
-        _typed(C, "C", (M, N), k.bits), *((None, 0) if workspace is None else _ws(workspace)), _stream_by(A, stream))
+        _typed(C, "C", (M, N), k.bits), *((None, 0) if workspace is None else _ws(workspace)),
+        _stream_by(A, stream, A_scale, W, W_scale, C, workspace))
     if rc < 0:
         _check(rc, "compass_fp8_gemm")
 
@@ -764,7 +776,8 @@ def compass_fp8_wgrad(dY, X8, X_scale, dW, workspace, accumulate: bool = False, 
     rc = (_lib or lib()).compass_fp8_wgrad(
         M, N, K, _kind(dW), _typed(dY, "dY", (M, N), k.bits), *_eight(X8, X_scale, "X8", (M, K), k),
         _typed(dW, "dW", (N, K), k.elements), 1 if accumulate else 0,
-        *((None, 0) if workspace is None else _ws(workspace)), _stream_by(dY, stream))
+        *((None, 0) if workspace is None else _ws(workspace)),
+        _stream_by(dY, stream, X8, X_scale, dW, workspace))
     if rc < 0:
         _check(rc, "compass_fp8_wgrad")
 
