@@ -127,6 +127,9 @@ constexpr Tile8 kGradTiles[kGradTileCount] = {
     {256, 256, 1, 1.43f, 1.50f, 9.5f}, {256, 128, 1, 0.90f, 0.94f, 5.3f}, {128, 128, 2, 0.64f, 1.04f, 3.9f},
     {128, 64, 2, 0.56f, 0.80f, 2.6f},  {64, 64, 3, 0.50f, 0.85f, 2.3f},
 };
+// Groups of 128 columns from the one that holds column k0 to the one that holds column
+// k0 + c. (A tile may start inside a group: behind an odd number of tiles of 64 columns.)
+__host__ __device__ inline int groups_from(int k0, int c) { return (k0 % 128 + c) / 128; }
 inline Cut plan_grad(int M, int N, int K) {
     return plan_cut(kGradTiles, kGradTileCount, N, K, (M + 63) / 64, 1, 4);
 }

@@ -64,7 +64,7 @@ struct XStage {
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             off[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.K + (uint32_t)c * 16u;
-            soff[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.S + (uint32_t)(c * 16 / kGroup);
+            soff[j] = (uint32_t)(row + j * STEP) * (uint32_t)p.S + (uint32_t)groups_from(k0, c * 16);
         }
         // 4 neighbouring lanes' first halves lie in every other chunk: the next 4 lanes
         // write their second ones with them, so that the 8 lanes that LDS takes at a
