@@ -420,8 +420,11 @@ class _Kinds:
         self.elements = (torch.bfloat16, torch.float32)
         self.float = (torch.float32,)
         self.index = (torch.int64,)
-        self.eight = (torch.float8_e4m3fn, torch.uint8)
-        self.scale = (torch.uint8, torch.float8_e8m0fnu)
+
+        def raw_or(name):   # (an older torch has no 8-bit types: the patterns alone)
+            t = getattr(torch, name, None)
+            return (torch.uint8,) if t is None else (torch.uint8, t)
+        self.eight, self.scale = raw_or("float8_e4m3fn"), raw_or("float8_e8m0fnu")
 
 
 _kinds = None
