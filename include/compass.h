@@ -419,7 +419,8 @@ int compass_fp8_scale_cols(int n, int *cols);
  * rows of K values; across = 1, the transposed, K rows of M values (groups along
  * M): a weight for the product of its backward pass. And back: x rounded once to
  * dtype; in bf16 a value as the operators here write it is exact down to 2^-126.
- * M up to 2^21, K up to 2^17. */
+ * M up to 2^21, K up to 2^17; back also M up to 2^17 with K up to 2^21, the rows that
+ * across writes (of which the products below take up to 2^17 values). */
 int compass_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across, void *x8, void *scale,
                       void *stream);
 int compass_fp8_dequant(int M, int K, int dtype, const void *x8, const void *scale, void *x, int64_t ldx,

@@ -171,12 +171,14 @@ __global__ __launch_bounds__(256) void dequant_kernel(const QuantParams p) {
 
 constexpr int kMaxRows = 1 << 21, kMaxCols = 1 << 17;
 
-int check(int M, int K, int dtype) {
+// Sizes of x; `either`: of 8-bit rows as they are written along x's rows or across them.
+int check(int M, int K, int dtype, bool either) {
     if (M < 1 || K < 1) return set_error(COMPASS_ERR_INVALID, "need positive M and K");
     if (dtype != COMPASS_BF16 && dtype != COMPASS_F32)
         return set_error(COMPASS_ERR_INVALID, "unknown element type %d", dtype);
-    if (M > kMaxRows || K > kMaxCols)
-        return set_error(COMPASS_ERR_UNSUPPORTED, "%d rows of %d elements, at most %d of %d", M, K, kMaxRows, kMaxCols);
+    if ((M > kMaxRows || K > kMaxCols) && !(either && M <= kMaxCols && K <= kMaxRows))
+        return set_error(COMPASS_ERR_UNSUPPORTED, "%d rows of %d elements, at most %d of %d%s", M, K, kMaxRows, kMaxCols,
+                         either ? " or the reverse" : "");
     return COMPASS_OK;
 }
 
@@ -203,7 +205,7 @@ int launched(const char *what) {
 }
 
 dim3 span_grid(int M, int K) {
-    const uint32_t items = (uint32_t)M * (uint32_t)((K + kSpan - 1) / kSpan);   // at most 2^21 2^8
+    const uint32_t items = (uint32_t)M * (uint32_t)((K + kSpan - 1) / kSpan);   // at most 2^21 2^8 or 2^17 2^12
     return dim3(std::min((items + 3) / 4, 1u << 22));
 }
 
@@ -219,7 +221,7 @@ int op_fp8_scale_cols(int K, int *cols) {
 
 int op_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across, void *x8, void *scale,
                  void *stream) {
-    int rc = check(M, K, dtype);
+    int rc = check(M, K, dtype, false);
     if (rc != COMPASS_OK) return rc;
     if (across != 0 && across != 1) return set_error(COMPASS_ERR_INVALID, "across = %d, must be 0 or 1", across);
     if ((rc = check_operands(x, ldx, K, dtype, x8, scale)) != COMPASS_OK) return rc;
@@ -255,7 +257,7 @@ int op_fp8_quant(int M, int K, int dtype, const void *x, int64_t ldx, int across
 }
 
 int op_fp8_dequant(int M, int K, int dtype, const void *x8, const void *scale, void *x, int64_t ldx, void *stream) {
-    int rc = check(M, K, dtype);
+    int rc = check(M, K, dtype, true);
     if (rc != COMPASS_OK) return rc;
     if ((rc = check_operands(x, ldx, K, dtype, x8, scale)) != COMPASS_OK) return rc;
     QuantParams p{};
