@@ -438,7 +438,9 @@ int compass_fp8_dequant(int M, int K, int dtype, const void *x8, const void *sca
  * h from elsewhere (NULL: none), with hh = h rstd and a = dy gamma:
  *   dx = dh + rstd (a - hh sum(a hh) / N), the gradient of x and of residual,
  *   dgamma = sum over rows of dy hh (N fp32; NULL: not wanted, and no workspace is needed).
- * dx may be dy, h or dh. All sums are fp32. */
+ * dx may be dy, h or dh. All sums are fp32: a row whose sum of h^2 passes fp32's largest
+ * (|h| around 1.8e19 / sqrt(N) and more) has rstd = 0 and y = 0, and with eps = 0 one whose
+ * squares are below its normal numbers (|h| under 1e-19) is inexact, of zeros NaN. */
 int compass_rms_forward(int M, int N, int dtype, int ptype, const void *x, int64_t ldx, const void *residual,
                         int64_t ldr, const void *gamma, float eps, void *h, int64_t ldh, void *y, int64_t ldy,
                         void *y8, void *scale, float *rstd, void *stream);

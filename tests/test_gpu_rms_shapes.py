@@ -89,6 +89,30 @@ def test_forward(dtype, threads, vectors, loose, N):
             _within("y8", v, ref, torch.maximum(ref.abs() * 2.0 ** -4, step * 2.0 ** -10) + 1.1 * ref.abs() * (rel + 4 * U24))
 
 
+def test_forward_at_the_ends_of_what_an_fp32_sum_holds():
+    torch = _torch()
+    N = 1024
+    x = _gen(5)(6, N)
+    x[0] *= 2.0 ** 55                  # inside: |h| up to 2^58, the sum below 2^126
+    x[1] = 2.0 ** 70                   # its square is beyond
+    x[2] = -2.0 ** 63 + 2.0 ** 40      # only the sum is
+    x[3] *= 2.0 ** -55                 # inside: squares from 2^-125
+    x[3][x[3].abs() < 2.0 ** -60] = 2.0 ** -58
+    x[4] = 0.0
+    y, rstd = torch.full((6, N), float("nan"), device="cuda"), torch.full((6,), float("nan"), device="cuda")
+    q = torch.full((6, N), 0x7F, dtype=torch.uint8, device="cuda")
+    s = torch.full((6, C.compass_fp8_scale_cols(N)), 255, dtype=torch.uint8, device="cuda")
+    C.compass_rms_forward(x, None, y, rstd, y8=q, scale=s, eps=0.0)
+    for m in (0, 3, 5):
+        want = 1.0 / torch.sqrt(x[m].double().square().mean())
+        _within("rstd", rstd[m], want, want * (N + 8) * U24)
+        _within("y", y[m], x[m].double() * want, (x[m].double() * want).abs() * (N + 13) * U24)
+    assert (rstd[1:3] == 0).all() and (y[1:3] == 0).all() and (q[1:3] & 127 == 0).all()
+    assert torch.isinf(rstd[4]) and torch.isnan(y[4]).all() and (q[4] & 127 == 127).all()
+    C.compass_rms_forward(x, None, y, rstd, y8=q, scale=s, eps=EPS)
+    assert (y[4] == 0).all() and (q[4] == 0).all() and torch.isfinite(rstd[3:]).all()
+
+
 def _check_backward(dy, h, gamma, rstd, dh, dtype):
     torch = _torch()
     M, N = h.shape
