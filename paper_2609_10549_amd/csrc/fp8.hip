@@ -54,7 +54,8 @@ __global__ __launch_bounds__(256) void quant_kernel(const QuantParams p) {
 // x (M x K) transposed: rows of K of M values, groups along M. A workgroup takes
 // 128 rows (a group) of 64 columns: each thread's vectors, the columns' largest
 // through LDS, then the bytes, turned in LDS to rows of 128. Bound by latency where
-// it is small: 500 x 1031 fp32 5.3 us.
+// it is small: 500 x 1031 fp32 5.3 us; a weight is close to memory's pace: 6144 x 12288
+// bf16 (226 MB) 46 to 54 us (4.6 TB/s; along the rows 41).
 template <class T, int V, bool LOOSE>
 __global__ __launch_bounds__(256) void quant_across_kernel(const QuantParams p) {
     constexpr int CV = 64 / V, RP = 256 / CV, PASSES = kGroup / RP;   // vectors per row, rows per pass

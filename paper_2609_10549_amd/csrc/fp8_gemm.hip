@@ -102,10 +102,12 @@ __device__ __forceinline__ void each_slot(const Step &step) {
 // stay and take a tile of every round; the next tile's first stages load under the
 // epilogue.
 //
-// What bounds it: the large tiles, the matrix cores at the clock that the power
-// allows. 8192 x 6144 x 12288 449 to 459 us from card to card (2.70 to 2.76 PFLOP/s; MFMA
-// busy 0.68 at 1.87 GHz; the library's product with one scale for all, 455 us on N(0, 1)
-// and 400 on these values). On the way there: a barrier per stage, loads in its last
+// What bounds it: the large tiles, the matrix cores and what feeds them. 8192 x 6144 x
+// 12288 445 to 462 us from card to card (2.7 PFLOP/s); MFMAs are busy in 0.59e6 of
+// 0.874e6 cycles, at 1.87 GHz (the library's product with one scale for all: 0.759e6
+// at 1.93; 455 us on N(0, 1) and 400 on these values). The rest is this kernel's own: where
+// the whole took 487 us it took 449 with scales that were constant, 391 without the
+// loads to LDS, 362 without either. On the way there: a barrier per stage, loads in its last
 // column of blocks and its scales by bytes 514 us; two barriers, the loads over half of
 // the stage 478; columns in pairs, scales by words of four stages, their addresses in
 // vector registers 466; a stage's place as the loads' scalar offset 459. What did not
@@ -113,8 +115,11 @@ __device__ __forceinline__ void each_slot(const Step &step) {
 // tiles in place of 4 (504 to 507) or of 8 (480 to 490), 192 x 256 tiles (575).
 //
 // Small products are bound by a tile's edges and, between one and two workgroups per
-// CU, by the CUs that have two: 777 x 5003 x 1552 16 us (280 tiles), 768 x 5120 x 1536 11
-// (240).
+// CU, by the CUs that have two: 777 x 5003 x 1552 16 us (280 tiles, 40 of them for 9 rows),
+// 768 x 5003 x 1552 13.5 (240), 768 x 5120 x 1536 11.6. Some rows against a long weight, by
+// the CUs without a tile or the fp32 slices that fill them: 64 x 6144 x 12288 23 us, 128
+// rows 26 (48 tiles in 5 slices), 256 rows 40 (96 in 2), 512 rows 59 (192 tiles), where
+// bytes and operations take 16, 16, 17 and 28.
 template <int BM, int BN, int WC, int NB, int WGS, bool PART>
 __global__ __launch_bounds__(kThreads, WGS) void product_kernel(const ProductParams p) {
     constexpr int WM = BM * WC / 4, WN = BN / WC, FM = WM / 16, FN = WN / 16, NM = FM * FN;

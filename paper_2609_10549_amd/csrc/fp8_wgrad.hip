@@ -130,9 +130,11 @@ __device__ __forceinline__ bf16x8 fragment(const R &r, uint32_t buf, int f) {
 // clock that the power allows, 1.25 to 1.35 PFLOP/s in whole rounds (8192 x 4096 x 4096
 // 203 to 219 us from card to card), and what X costs beside them, 0.2 of the time
 // (without its conversion and loads 0.8; a conversion is a slow operation). 8192 x 6144 x
-// 12288 973 to 1010 us: 4.5 rounds of 256 x 256 tiles, three of them and three of 256 x
-// 128. Few rows: dW's stores, 64 x 6144 x 12288 45 us (3.4 TB/s). Between them latency: 777
-// x 5000 x 1552 26 to 30 us, two rounds of 13 stages. What did not help: conversions over
+// 12288 973 to 1035 us: 4.5 rounds of 256 x 256 tiles, three of them and three of 256 x
+// 128; added to what dW holds, which the epilogue reads as it stores, 85 to 95 us more. Few
+// rows: dW's stores, 64 x 6144 x 12288 45 us (3.4 TB/s). Between them latency: 777 x 5000 x
+// 1552 30 us (added to dW 32), two rounds of 13 stages, each of which waits for loads that
+// are less than a stage old. What did not help: conversions over
 // three quarters of a stage in place of a half, the barrier later, three or four
 // workgroups of the small tiles per CU in place of two and three (26.9 -> 28.8), 64 x 128
 // tiles for 128 x 64 (31), 192 x 256 tiles (1011).

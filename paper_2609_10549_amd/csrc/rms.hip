@@ -45,7 +45,9 @@ struct RmsParams {
 //
 // Bound by memory: 32768 x 8192 bf16 with the residual (2.15 GB) 364 us (5.9 TB/s);
 // 8192 x 12288 bf16 with the residual to 8 bits (0.70 GB) 130 us (5.4 TB/s). Single
-// tokens (4 x 12288): 4.8 us, one row after another through a workgroup's barriers.
+// tokens are bound by latency, the loads, the sum over a workgroup's waves and the
+// stores of a row one after another: 1 x 12288 4.1 us, 4 rows 4.6 to 4.8, 256 (one
+// per CU) 6.0.
 template <class T, int V, bool LOOSE, int TPR, int ITEMS, bool EIGHT>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rms_forward_kernel(const RmsParams p) {
     constexpr int THREADS = TPR < 256 ? 256 : TPR;
@@ -111,7 +113,10 @@ constexpr int backward_threads(int tpr) { return tpr > 512 ? tpr : tpr % 192 == 
 // workgroups keep that traffic small).
 //
 // Bound by memory: 8192 x 12288 bf16 with dh (805 MB) 151 us (5.3 TB/s), the join of
-// the sums 5; 1000 x 4097 fp32 16.4 us, four rows one after another per workgroup.
+// the sums 5. Lengths whose registers hold no row ahead, with the join: 8192 x 4096 56 us
+// (4.8 TB/s), 8192 x 8192 105 (5.1). Few rows, latency: 2048 x 4096 19 us with the join
+// (3.5 TB/s); 1000 x 4097 fp32 16.4, four rows one after another per workgroup, whose
+// 1536 places take 1025 vectors.
 template <class T, int V, bool LOOSE, int TPR, int ITEMS>
 __global__ __launch_bounds__(backward_threads(TPR)) void rms_backward_kernel(const RmsParams p) {
     constexpr int THREADS = backward_threads(TPR), ROWS = THREADS / TPR, WAVES = TPR / 64;
