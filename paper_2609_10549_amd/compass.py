@@ -464,14 +464,19 @@ def _not_a_tensor(what: str) -> ValueError:
     return ValueError(f"{what}: must be a tensor (its sizes are read)")
 
 
+_SIZE_MAX = (1 << 31) - 1   # of the entry points' int arguments, which ctypes cuts to 32 bits without a word
+
+
 def _dims(x, what: str, n: int = 2) -> tuple:
-    """The sizes of x, a tensor of n dimensions."""
+    """The sizes of x, a tensor of n dimensions (1 or 2)."""
     try:
         shape = x.shape
     except AttributeError:
         raise _not_a_tensor(what) from None
     if len(shape) != n:
         raise ValueError(f"{what}: shape {_shape_of(x)}, expected {n} dimensions")
+    if shape[0] > _SIZE_MAX or shape[-1] > _SIZE_MAX:
+        raise ValueError(f"{what}: shape {_shape_of(x)}, a size beyond 2^31 - 1")
     return shape
 
 
@@ -632,9 +637,7 @@ def compass_embed_backward(ids, dy, dtable, workspace, scale: float = 1.0, v0: i
 # ---------------------------------------------- the MLP in 8 bits (see the header)
 def compass_fp8_scale_cols(n: int) -> int:
     """Bytes of the scales of a row of n 8-bit values."""
-    out = ctypes.c_int()
-    _check(lib().compass_fp8_scale_cols(n, ctypes.byref(out)), "compass_fp8_scale_cols")
-    return out.value
+    return _sizes("compass_fp8_scale_cols", n, out=ctypes.c_int())
 
 
 def _eight(x, scale, what: str, shape: tuple, k: _Kinds) -> tuple:
@@ -675,8 +678,11 @@ def _stream_by(x, stream, *others) -> int | None:
     return stream.cuda_stream
 
 
-def _sizes(name: str, *sizes) -> int:
-    out = ctypes.c_size_t()
+def _sizes(name: str, *sizes, out=None) -> int:
+    """What the entry point `name` answers for these sizes."""
+    if max(map(abs, sizes)) > _SIZE_MAX:
+        raise ValueError(f"{name}: {', '.join(map(str, sizes))}, a size beyond 2^31 - 1")
+    out = ctypes.c_size_t() if out is None else out
     _check(getattr(lib(), name)(*sizes, ctypes.byref(out)), name)
     return out.value
 
