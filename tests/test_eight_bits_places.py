@@ -1,6 +1,6 @@
 """Where the operands of the MLP in 8 bits lie: each of them, and the stream, on the
-current GPU (no GPU; every call here is refused before the library is reached, or
-reaches a library that only counts)."""
+current GPU. Without one, every call here is refused before the library is reached, or
+reaches a library that only counts."""
 import pytest
 
 from paper_2609_10549_amd import compass as C
@@ -73,3 +73,20 @@ def test_operands_that_are_absent_or_addresses_have_no_place(monkeypatch):
     gemm = calls[C.compass_fp8_gemm]
     C.compass_fp8_gemm(**{**gemm, "A_scale": 4096, "C": 8192, "workspace": None}, stream=0)
     assert len(reached) == 3
+
+
+@pytest.mark.gpu
+def test_streams_of_the_current_gpu_are_taken():
+    import torch
+    x = torch.arange(1, 601, device="cuda").view(2, 300).float()
+    q, s = torch.empty(2, 300, dtype=torch.uint8, device="cuda"), torch.empty(2, 4, dtype=torch.uint8, device="cuda")
+    C.compass_fp8_quant(x, q, s)
+    want = q.clone(), s.clone()
+    own = torch.cuda.Stream()
+    streams = [own, own.cuda_stream, torch.cuda.ExternalStream(own.cuda_stream), torch.cuda.default_stream(), torch.cuda.current_stream()]
+    for stream in streams:
+        q.zero_(), s.zero_()
+        torch.cuda.synchronize()
+        C.compass_fp8_quant(x, q, s, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(q, want[0]) and torch.equal(s, want[1])
